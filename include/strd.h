@@ -410,6 +410,78 @@ int strd_attn_decode_step(const void *q, const void *k_cache, const void *v_cach
                           int Hkv, int d, float scale, strd_dtype io, void *ws, size_t ws_bytes, void *stream);
 
 /* ---------------------------------------------------------------------------
+ * Serving what a reduced prefill keeps: attention over packed sequences with changed scores, a cache in 4 bits, decode steps
+ * that gather attention weights, and eviction by them.
+ *
+ * Scores.  With x = scale * q_t^h . k_j, in this order:
+ *     cap > 0:    x = cap * tanh(x / cap)                      (cap = 0: no cap)
+ *     slopes:     x = x - slopes[h] * |pos[t] - pos[j]|        (NULL: no bias)
+ *   slopes [dev] [Hq] fp32, any finite numbers; pos [dev] int32, a position per row (after a compaction the rows' old
+ *   positions: pos_out of strd_compact), taken as fp32 numbers (exact below 2^24); NULL: the row's number in its sequence.
+ * cap must be finite and >= 0, else STRD_EINVAL.
+ *
+ * attn_prefill_varlen -- strd_attn_prefill for a packed batch (strd_seq above; K is not looked at, N and M may be 0, and so may a
+ * sequence's rows altogether): a row attends to rows of its own sequence only,
+ *     to those up to itself; with prefix != 0 a vision row to every vision row of its sequence instead.
+ *   q [dev] [rows, Hq, d], k, v [dev] [rows, Hkv, d] with row pitches ldq, ldk, ldv in elements (>= a row's own), so that they may
+ *   be column ranges of one projection; o [dev] [rows, Hq, d], contiguous.  Rows behind the last sequence are neither read nor
+ *   written.  What a row does not see does not reach it, values that are not finite included.  pos holds one number per row.
+ *   bf16 with d in {64, 128}, 16-byte aligned tensors and pitches that are multiples of 8 go to the matrix cores
+ *   (strd_attn_prefill_varlen_kernel_path), d <= 256 otherwise; no workspace.  Hq % Hkv == 0, scale > 0, 1 <= nseq <=
+ *   STRD_VARLEN_MAX, at most 2^30 rows.
+ *
+ * The 4-bit cache.  A row of keys (or values) of one kv head is cut into groups of 32 channels.  A group is 32 codes n in 0..15,
+ * channel 2 i in the low half of byte i, channel 2 i + 1 in the high half, and two bf16 numbers s, z; a code stands for
+ * z + s (n - 8).  With lo, hi the smallest and the largest of the 32 and fp32 arithmetic: s = bf16((hi - lo) / 15), 0 if below
+ * 2^-100; z = bf16(lo + 8 s); n = clamp(rint((x - z) / s) + 8, 0, 15), ties to even.  A value is off by s / 2 and the rounding of s and z
+ * at most (|z| 2^-9 + s / 16).  A group with a value that is not finite, or whose s or z is not, reads back as NaN.
+ *   k_codes, v_codes [dev] [rows, Hkv, d / 2] bytes    k_meta, v_meta [dev] [rows, Hkv, d / 32, 2] bf16 (s, z)
+ * all 16-byte aligned (else STRD_EINVAL); d a multiple of 32 up to 256 (else STRD_EUNSUPPORTED).  They compact as any other tensor.
+ *   kv4_store: rows row0 .. row0 + R - 1 of the cache from k, v [dev] [R, Hkv, d] with row pitches ldk, ldv (elements); the
+ *              other rows are left as they are.  R = 0 allowed.
+ *   kv4_load:  k, v [dev] [R, Hkv, d] (contiguous, 32-byte aligned) from rows row0 ..; values rounded once to io.
+ * rows (the cache's capacity) bounds row0 + R: STRD_EINVAL beyond it.
+ *
+ * attn_decode_step_kv4, attn_decode_step_weights -- strd_attn_decode_step with changed scores over the first T rows of a 4-bit or of a
+ * plain cache (the newest token's own row is the last), and the attention weight that each row has gathered:
+ *     w_out[j] = (w_in ? w_in[j] : 0) + 1/Hq * sum_h softmax_j(x^h)
+ *   w_in, w_out [dev] [T] fp32; w_out may be w_in; w_out NULL: no weights (w_in must then be NULL).  The token's position is
+ *   pos[T - 1].  d <= 256, any Hq % Hkv == 0; io is the type of q, o and of a plain cache.  Workspace [dev], 16-byte aligned:
+ *   *_workspace bytes (STRD_EWORKSPACE otherwise); `weights`: whether w_out is wanted.  Deterministic.
+ *
+ * cache_evict -- keeps K of T rows: the first `first`, the last `last`, and of those between the K - first - last with the
+ * largest weights (ties to the lowest row; NaN and negative weights as in strd_select_topk), in their old order.
+ *   w [dev] [T] fp32, 16-byte aligned        idx [dev] [K] int32 output, ascending
+ *   items [host] [n_items], n_items <= STRD_COMPACT_MAX - 1: tensors of T rows cut down to K rows, by the rules of strd_compact
+ *   w_out [dev] [K] fp32 or NULL: the kept rows' weights     pos_out [dev] [K] int32 or NULL: pos_in of the kept rows (NULL: idx)
+ *   None of the outputs may overlap an input.  first, last >= 0, first + last <= K, 1 <= K <= T <= 2^30, else STRD_EINVAL.
+ *   Workspace [dev]: strd_cache_evict_workspace bytes.  Bit-exact and deterministic.
+ *
+ * All asynchronous on `stream`; no call allocates.
+ * ------------------------------------------------------------------------- */
+int strd_attn_prefill_varlen_kernel_path(int Hq, int Hkv, int d, strd_dtype io);
+int strd_attn_prefill_varlen(const void *q, int64_t ldq, const void *k, int64_t ldk, const void *v, int64_t ldv, void *o,
+                             const strd_seq *seqs, int nseq, int prefix, float cap, const float *slopes, const int32_t *pos, int Hq,
+                             int Hkv, int d, float scale, strd_dtype io, void *stream);
+typedef struct {
+    void *k_codes, *k_meta, *v_codes, *v_meta;
+} strd_kv4;
+int strd_kv4_store(const void *k, int64_t ldk, const void *v, int64_t ldv, const strd_kv4 *cache, int rows, int row0, int R, int Hkv, int d,
+                   strd_dtype io, void *stream);
+int strd_kv4_load(const strd_kv4 *cache, int rows, int row0, int R, void *k, void *v, int Hkv, int d, strd_dtype io, void *stream);
+size_t strd_attn_decode_step_kv4_workspace(int T, int Hq, int Hkv, int d, int weights, strd_dtype io);
+int strd_attn_decode_step_kv4(const void *q, const strd_kv4 *cache, void *o, int T, int Hq, int Hkv, int d, float scale, float cap,
+                              const float *slopes, const int32_t *pos, const float *w_in, float *w_out, strd_dtype io, void *ws,
+                              size_t ws_bytes, void *stream);
+size_t strd_attn_decode_step_weights_workspace(int T, int Hq, int Hkv, int d, int weights, strd_dtype io);
+int strd_attn_decode_step_weights(const void *q, const void *k_cache, const void *v_cache, void *o, int T, int Hq, int Hkv, int d,
+                                  float scale, float cap, const float *slopes, const int32_t *pos, const float *w_in, float *w_out,
+                                  strd_dtype io, void *ws, size_t ws_bytes, void *stream);
+size_t strd_cache_evict_workspace(int T, int K, int first, int last);
+int strd_cache_evict(const float *w, int T, int K, int first, int last, const strd_compact_item *items, int n_items,
+                     const int32_t *pos_in, int32_t *pos_out, int32_t *idx, float *w_out, void *ws, size_t ws_bytes, void *stream);
+
+/* ---------------------------------------------------------------------------
  * schedule_budgets -- per-layer token budgets of a retention schedule (Sec. 3.2
  * and App. "Reduction Schedule Configurations").  alpha_l is relative to the
  * original count N0; budgets never grow with depth and never fall below

@@ -10,6 +10,7 @@ from .binding import (  # noqa: F401
     score_attn, score_mamba, score_mamba_full, select_topk, ssd_prefill, ssd_prefill_gather,
     select_topk_noalloc, kernel_path, PATH_NONE, PATH_MFMA, PATH_SIMT,
     score_attn_varlen, score_mamba_varlen, select_topk_varlen, compact_varlen, mfma_rate_probe,
+    Kv4Cache, attn_prefill_varlen, kv4_store, kv4_load, attn_decode_step_kv4, attn_decode_step_weights, cache_evict,
 )
 
 __all__ = [
@@ -17,5 +18,6 @@ __all__ = [
     "ssd_prefill", "ssd_prefill_gather", "attn_prefill", "schedule_budgets", "schedule_sigmoid", "schedule_step_decay",
     "linear", "linear_mfma", "linear_library", "linear_mfma_supported", "rmsnorm", "gated_rmsnorm", "conv1d_silu", "softplus_dt", "avgpool", "ssd_decode_step", "attn_decode_step",
     "score_attn_varlen", "score_mamba_varlen", "select_topk_varlen", "compact_varlen", "mfma_rate_probe",
+    "Kv4Cache", "attn_prefill_varlen", "kv4_store", "kv4_load", "attn_decode_step_kv4", "attn_decode_step_weights", "cache_evict",
     "select_topk_noalloc", "kernel_path", "PATH_NONE", "PATH_MFMA", "PATH_SIMT", "schedule_named", "hybrid_layout", "HYBRID_LAYERS", "LAYER_MAMBA", "LAYER_MLP", "LAYER_ATTN", "NAMED_SCHEDULES",
 ]

@@ -10,7 +10,7 @@ from __future__ import annotations
 import ctypes
 import importlib.util
 import os
-from typing import Optional, Sequence, Tuple
+from typing import NamedTuple, Optional, Sequence, Tuple
 
 import torch
 
@@ -67,6 +67,16 @@ _SIGNATURES = {
     "strd_ssd_decode_step": (_int, [_vp] * 8 + [_int] * 4 + [_int, _vp]),
     "strd_attn_decode_step_workspace": (_c.c_size_t, [_int, _int, _int, _int, _int]),
     "strd_attn_decode_step": (_int, [_vp, _vp, _vp, _vp, _int, _int, _int, _int, _f32, _int, _vp, _c.c_size_t, _vp]),
+    "strd_attn_prefill_varlen_kernel_path": (_int, [_int] * 4),
+    "strd_attn_prefill_varlen": (_int, [_vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _int, _int, _f32, _vp, _vp] + [_int] * 3 + [_f32, _int, _vp]),
+    "strd_kv4_store": (_int, [_vp, _i64, _vp, _i64, _vp] + [_int] * 6 + [_vp]),
+    "strd_kv4_load": (_int, [_vp, _int, _int, _int, _vp, _vp, _int, _int, _int, _vp]),
+    "strd_attn_decode_step_kv4_workspace": (_sz, [_int] * 6),
+    "strd_attn_decode_step_kv4": (_int, [_vp] * 3 + [_int] * 4 + [_f32, _f32] + [_vp] * 4 + [_int, _vp, _sz, _vp]),
+    "strd_attn_decode_step_weights_workspace": (_sz, [_int] * 6),
+    "strd_attn_decode_step_weights": (_int, [_vp] * 4 + [_int] * 4 + [_f32, _f32] + [_vp] * 4 + [_int, _vp, _sz, _vp]),
+    "strd_cache_evict_workspace": (_sz, [_int] * 4),
+    "strd_cache_evict": (_int, [_vp, _int, _int, _int, _int, _vp, _int, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
     "strd_schedule_budgets": (_int, [_vp, _int, _int, _int, _vp]),
     "strd_schedule_sigmoid": (_int, [_int, _c.c_double, _c.c_double, _c.c_double, _c.c_double, _vp]),
     "strd_schedule_step_decay": (_int, [_vp, _vp, _vp, _int, _int, _vp]),
@@ -341,6 +351,69 @@ def attn_decode_step(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tens
     """The newest token's attention over the T cached rows (its own included): q [Hq,d],
     k_cache, v_cache [T,Hkv,d]; returns o [Hq,d]."""
     return (_host or host()).attn_decode_step(q, k_cache, v_cache, scale, ws)
+
+
+# ---- serving the rows that a reduced prefill keeps ------------------------------------------
+class Kv4Cache(NamedTuple):
+    """Keys and values of `rows` tokens in 4 bits (the format: include/strd.h): codes uint8 [rows, Hkv, d/2], meta bf16
+    [rows, Hkv, d/32, 2].  The four tensors compact, slice and copy by rows like any other."""
+    k_codes: torch.Tensor
+    k_meta: torch.Tensor
+    v_codes: torch.Tensor
+    v_meta: torch.Tensor
+
+    @classmethod
+    def empty(cls, rows: int, Hkv: int, d: int, device="cuda") -> "Kv4Cache":
+        if d % 32:
+            raise StrdError("a 4-bit cache needs heads of a multiple of 32 channels")
+        codes = [torch.empty((rows, Hkv, d // 2), dtype=torch.uint8, device=device) for _ in range(2)]
+        meta = [torch.empty((rows, Hkv, d // 32, 2), dtype=torch.bfloat16, device=device) for _ in range(2)]
+        return cls(codes[0], meta[0], codes[1], meta[1])
+
+
+def attn_prefill_varlen(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seqs, prefix: bool = False, cap: float = 0.0,
+                        slopes: Optional[torch.Tensor] = None, pos: Optional[torch.Tensor] = None,
+                        scale: Optional[float] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Causal GQA attention of a packed batch, every sequence on its own: o [rows,Hq,d].  q, k, v may be column ranges of a wider
+    matrix.  prefix: vision rows see every vision row of their sequence.  cap > 0: scores become cap * tanh(score / cap);
+    slopes [Hq] fp32: they fall by slopes[h] times the distance of the rows' pos [rows] int32 (None: row numbers)."""
+    return (_host or host()).attn_prefill_varlen(q, k, v, seqs, prefix, cap, slopes, pos, scale, out)
+
+
+def kv4_store(k: torch.Tensor, v: torch.Tensor, cache: Kv4Cache, row0: int) -> None:
+    """k, v [R,Hkv,d] into rows row0 .. row0 + R - 1 of a 4-bit cache."""
+    return (_host or host()).kv4_store(k, v, cache, row0)
+
+
+def kv4_load(cache: Kv4Cache, row0: int, R: int, dtype: torch.dtype = torch.bfloat16) -> Tuple[torch.Tensor, torch.Tensor]:
+    """What rows row0 .. row0 + R - 1 of a 4-bit cache stand for: k, v [R,Hkv,d]."""
+    return (_host or host()).kv4_load(cache, row0, R, dtype)
+
+
+def attn_decode_step_kv4(q: torch.Tensor, cache: Kv4Cache, T: int, scale: Optional[float] = None, cap: float = 0.0,
+                         slopes: Optional[torch.Tensor] = None, pos: Optional[torch.Tensor] = None,
+                         weights: Optional[torch.Tensor] = None, weights_out: Optional[torch.Tensor] = None,
+                         want_weights: bool = True, ws: Optional[torch.Tensor] = None):
+    """The newest token's attention over the first T rows of a 4-bit cache (its own included): returns o [Hq,d] and, if wanted,
+    weights [T] fp32 plus the mean over the heads of this step's attention weights (weights_out may be `weights`)."""
+    return (_host or host()).attn_decode_step_kv4(q, cache, T, scale, cap, slopes, pos, weights, weights_out, want_weights, ws)
+
+
+def attn_decode_step_weights(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, scale: Optional[float] = None,
+                             cap: float = 0.0, slopes: Optional[torch.Tensor] = None, pos: Optional[torch.Tensor] = None,
+                             weights: Optional[torch.Tensor] = None, weights_out: Optional[torch.Tensor] = None,
+                             want_weights: bool = True, ws: Optional[torch.Tensor] = None):
+    """The same over a plain cache k_cache, v_cache [T,Hkv,d]."""
+    return (_host or host()).attn_decode_step_weights(q, k_cache, v_cache, scale, cap, slopes, pos, weights, weights_out,
+                                                      want_weights, ws)
+
+
+def cache_evict(weights: torch.Tensor, K: int, first: int, last: int, tensors: Sequence[torch.Tensor],
+                pos: Optional[torch.Tensor] = None, outs: Optional[Sequence[torch.Tensor]] = None,
+                ws: Optional[torch.Tensor] = None):
+    """Keep K of the T rows of `tensors`: the first `first`, the last `last` and the heaviest between, in order.  Returns (idx [K]
+    int32, the kept rows' weights, the cut-down tensors, the kept rows' pos or None)."""
+    return (_host or host()).cache_evict(weights, K, first, last, tensors, pos, outs, ws)
 
 
 def schedule_budgets(alpha: Sequence[float], N0: int, K_min: int = 0):

@@ -6,7 +6,8 @@
 
 #include <algorithm>
 
-#include "common.h"
+#include "attn_decode_cache.h"
+#include "attn_varlen.h"
 
 using namespace strd;
 
@@ -495,6 +496,147 @@ int strd_attn_decode_step(const void *q, const void *k_cache, const void *v_cach
     const size_t need = attn_decode_workspace(T, Hq, Hkv, d);
     if (!ws || ws_bytes < need || (uintptr_t)ws % 16) return STRD_EWORKSPACE;
     return attn_decode_launch(q, k_cache, v_cache, o, T, Hq, Hkv, d, scale, io, (float *)ws, as_stream(stream));
+}
+
+// ------------------------------------------------------------------ packed attention, caches -
+namespace {
+constexpr int kMostRows = 1 << 30;
+inline bool cap_ok(float cap) { return cap >= 0.f && cap < INFINITY; }
+
+// Sequences with rows, longest first, in blocks of `bm` rows; false if the descriptors are inconsistent.
+bool plan_attn(const strd_seq *seqs, int nseq, int bm, AttnTab &t, long long &rows, long long &units) {
+    if (!seqs || nseq < 1 || nseq > STRD_VARLEN_MAX) return false;
+    int order[STRD_VARLEN_MAX], n = 0;
+    long long row0[STRD_VARLEN_MAX];
+    rows = units = 0;
+    for (int b = 0; b < nseq; ++b) {
+        if (seqs[b].N < 0 || seqs[b].M < 0) return false;
+        row0[b] = rows;
+        rows += (long long)seqs[b].N + seqs[b].M;
+        if (rows > kMostRows) return false;
+        if (seqs[b].N + seqs[b].M > 0) order[n++] = b;
+    }
+    std::stable_sort(order, order + n, [&](int a, int b) { return seqs[a].N + seqs[a].M > seqs[b].N + seqs[b].M; });
+    t = AttnTab();
+    t.nseq = n;
+    for (int i = 0; i < n; ++i) {
+        const strd_seq &s = seqs[order[i]];
+        t.row0[i] = (int)row0[order[i]];
+        t.len[i] = s.N + s.M;
+        t.vis[i] = s.N;
+        t.nb[i] = ceil_div(t.len[i], bm);
+        if (i) units += (long long)(t.nb[i - 1] - t.nb[i]) * i;
+        t.base[i] = (int)std::min(units, (long long)kMostRows);
+    }
+    if (n) units += (long long)t.nb[n - 1] * n;
+    return true;
+}
+
+int decode_cache_call(DecCall &a, float scale, float cap, const float *slopes, const int32_t *pos, void *ws, size_t ws_bytes, void *stream) {
+    if (a.T < 1 || a.T > kMostRows || a.Hq < 1 || a.Hkv < 1 || a.d < 1 || a.Hq % a.Hkv || !io_ok(a.io) || !(scale > 0.f) || !cap_ok(cap) || !a.q ||
+        !a.c.k || !a.c.v || !a.o || (a.w_in && !a.w_out) || (a.kv4 && (!a.c.km || !a.c.vm)))
+        return STRD_EINVAL;
+    if (a.d > 256 || (a.kv4 && a.d % kKv4Group) || a.Hkv > 65535 || a.Hq > (1 << 20)) return STRD_EUNSUPPORTED;
+    if (a.kv4 && !aligned16(a.c.k, a.c.km, a.c.v, a.c.vm)) return STRD_EINVAL;
+    const size_t need = attn_decode_cache_ws(a.T, a.Hq, a.Hkv, a.d, a.kv4, a.w_out != nullptr, a.io);
+    if (!ws || ws_bytes < need || !aligned16(ws)) return STRD_EWORKSPACE;
+    a.mod = {scale, cap, cap > 0.f ? 1.f / cap : 0.f, slopes, pos};
+    return attn_decode_cache(a, ws, as_stream(stream));
+}
+}  // namespace
+
+int strd_attn_prefill_varlen_kernel_path(int Hq, int Hkv, int d, strd_dtype io) {
+    if (Hq < 1 || Hkv < 1 || d < 1 || Hq % Hkv || !io_ok(io)) return STRD_PATH_NONE;
+    return attn_general_supported(d) ? STRD_PATH_SIMT : STRD_PATH_NONE;
+}
+
+int strd_attn_prefill_varlen(const void *q, int64_t ldq, const void *k, int64_t ldk, const void *v, int64_t ldv, void *o,
+                             const strd_seq *seqs, int nseq, int prefix, float cap, const float *slopes, const int32_t *pos, int Hq,
+                             int Hkv, int d, float scale, strd_dtype io, void *stream) {
+    AttnMod m;
+    long long rows, units;
+    if (Hq < 1 || Hkv < 1 || d < 1 || Hq % Hkv || !io_ok(io) || !(scale > 0.f) || !cap_ok(cap) || !plan_attn(seqs, nseq, 16, m.tab, rows, units) ||
+        ldq < (int64_t)Hq * d || ldk < (int64_t)Hkv * d || ldv < (int64_t)Hkv * d || (rows > 0 && (!q || !k || !v || !o)))
+        return STRD_EINVAL;
+    if (rows == 0) return STRD_OK;
+    m.ldq = ldq, m.ldk = ldk, m.ldv = ldv;
+    m.scale = scale, m.cap = cap, m.inv_cap = cap > 0.f ? 1.f / cap : 0.f;
+    m.slopes = slopes, m.pos = pos, m.prefix = prefix != 0;
+    if (!attn_general_supported(d)) return STRD_EUNSUPPORTED;
+    return attn_varlen_general(q, k, v, o, Hq, Hkv, d, m, units, io, as_stream(stream));
+}
+
+namespace {
+bool kv4_ok(const strd_kv4 *c, int rows, int row0, int R, int Hkv, int d, strd_dtype io) {
+    return c && rows >= 0 && row0 >= 0 && R >= 0 && (long long)row0 + R <= rows && rows <= kMostRows && Hkv >= 1 && d >= 1 && io_ok(io) &&
+           (R == 0 || (c->k_codes && c->k_meta && c->v_codes && c->v_meta && aligned16(c->k_codes, c->k_meta, c->v_codes, c->v_meta)));
+}
+bool kv4_takes(int R, int Hkv, int d) { return d % kKv4Group == 0 && d <= 256 && (long long)R * Hkv * (d / 8) <= 256LL * 0x7FFFFFFF; }
+}  // namespace
+
+int strd_kv4_store(const void *k, int64_t ldk, const void *v, int64_t ldv, const strd_kv4 *cache, int rows, int row0, int R, int Hkv, int d,
+                   strd_dtype io, void *stream) {
+    if (!kv4_ok(cache, rows, row0, R, Hkv, d, io) || (R > 0 && (!k || !v)) || ldk < (int64_t)Hkv * d || ldv < (int64_t)Hkv * d) return STRD_EINVAL;
+    if (!kv4_takes(R, Hkv, d)) return STRD_EUNSUPPORTED;
+    if (R == 0) return STRD_OK;
+    return kv4_store_launch(k, ldk, v, ldv, *cache, row0, R, Hkv, d, io, as_stream(stream));
+}
+
+int strd_kv4_load(const strd_kv4 *cache, int rows, int row0, int R, void *k, void *v, int Hkv, int d, strd_dtype io, void *stream) {
+    if (!kv4_ok(cache, rows, row0, R, Hkv, d, io) || (R > 0 && (!k || !v)) || (((uintptr_t)k | (uintptr_t)v) & 31)) return STRD_EINVAL;
+    if (!kv4_takes(R, Hkv, d)) return STRD_EUNSUPPORTED;
+    if (R == 0) return STRD_OK;
+    return kv4_load_launch(*cache, row0, R, k, v, Hkv, d, io, as_stream(stream));
+}
+
+size_t strd_attn_decode_step_kv4_workspace(int T, int Hq, int Hkv, int d, int weights, strd_dtype io) {
+    if (T < 1 || T > kMostRows || Hq < 1 || Hkv < 1 || d < 1 || Hq % Hkv) return 0;
+    return attn_decode_cache_ws(T, Hq, Hkv, d, true, weights != 0, io);
+}
+size_t strd_attn_decode_step_weights_workspace(int T, int Hq, int Hkv, int d, int weights, strd_dtype io) {
+    if (T < 1 || T > kMostRows || Hq < 1 || Hkv < 1 || d < 1 || Hq % Hkv) return 0;
+    return attn_decode_cache_ws(T, Hq, Hkv, d, false, weights != 0, io);
+}
+
+int strd_attn_decode_step_kv4(const void *q, const strd_kv4 *cache, void *o, int T, int Hq, int Hkv, int d, float scale, float cap,
+                              const float *slopes, const int32_t *pos, const float *w_in, float *w_out, strd_dtype io, void *ws,
+                              size_t ws_bytes, void *stream) {
+    if (!cache) return STRD_EINVAL;
+    DecCall a = {q, {cache->k_codes, cache->k_meta, cache->v_codes, cache->v_meta}, o, T, Hq, Hkv, d, {}, w_in, w_out, io, true};
+    return decode_cache_call(a, scale, cap, slopes, pos, ws, ws_bytes, stream);
+}
+int strd_attn_decode_step_weights(const void *q, const void *k_cache, const void *v_cache, void *o, int T, int Hq, int Hkv, int d,
+                                  float scale, float cap, const float *slopes, const int32_t *pos, const float *w_in, float *w_out,
+                                  strd_dtype io, void *ws, size_t ws_bytes, void *stream) {
+    DecCall a = {q, {k_cache, nullptr, v_cache, nullptr}, o, T, Hq, Hkv, d, {}, w_in, w_out, io, false};
+    return decode_cache_call(a, scale, cap, slopes, pos, ws, ws_bytes, stream);
+}
+
+size_t strd_cache_evict_workspace(int T, int K, int first, int last) {
+    if (T < 1 || K < 1 || K > T || first < 0 || last < 0 || (long long)first + last > K) return 0;
+    return select_topk_ws(T - last);
+}
+
+int strd_cache_evict(const float *w, int T, int K, int first, int last, const strd_compact_item *items, int n_items,
+                     const int32_t *pos_in, int32_t *pos_out, int32_t *idx, float *w_out, void *ws, size_t ws_bytes, void *stream) {
+    if (!w || !idx || T < 1 || T > kMostRows || K < 1 || K > T || first < 0 || last < 0 || (long long)first + last > K || !aligned16(w, ws))
+        return STRD_EINVAL;
+    if (n_items < 0 || n_items > STRD_COMPACT_MAX - 1 || (n_items > 0 && !items)) return STRD_EINVAL;
+    strd_compact_item all[STRD_COMPACT_MAX];
+    bool large = false;  // more than the gather's grid reaches: known before the selection is launched
+    for (int i = 0; i < n_items; ++i) {
+        if (!items[i].src || !items[i].dst || items[i].row_bytes <= 0 || items[i].row_bytes % 4) return STRD_EINVAL;
+        large |= items[i].row_bytes > 1 << 28 || items[i].row_bytes * K > 1LL << 37;
+        all[i] = items[i];
+    }
+    if (large) return STRD_EUNSUPPORTED;
+    if (w_out) all[n_items] = {w, w_out, sizeof(float)};
+    const size_t need = select_topk_ws(T - last);
+    if (need && (!ws || ws_bytes < need)) return STRD_EWORKSPACE;
+    const int rc = select_kept_launch(w, T, K, first, last, idx, ws, as_stream(stream));
+    if (rc != STRD_OK) return rc;
+    const int n = n_items + (w_out ? 1 : 0);
+    return n || pos_out ? compact_launch(all, n, idx, T, 0, K, pos_in, pos_out, as_stream(stream)) : STRD_OK;
 }
 
 // ------------------------------------------------------------------ schedules (host) -------

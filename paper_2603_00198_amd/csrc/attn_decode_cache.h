@@ -1,0 +1,52 @@
+// What the decode steps over a cache with capped or biased scores and gathered weights share.
+#pragma once
+#include "kv4.h"
+
+namespace strd {
+
+constexpr int kDecMaxSplits = 512;
+constexpr float kDecNegBig = -3.0e38f;
+
+// x = scale * q.k -> score: the cap first, then the bias (see strd.h).
+struct ScoreMod {
+    float scale, cap, inv_cap;      // cap == 0: none
+    const float *slopes;            // [Hq] or null
+    const int32_t *pos;             // [T] or null: the row number
+};
+// In units of log2 e.  tanhf and not an exponential form: the scores' errors are the weights' relative errors.
+__device__ __forceinline__ float capped_score(const ScoreMod &m, float dot) {
+    const float x = dot * m.scale;
+    return m.cap > 0.f ? m.cap * tanhf(x * m.inv_cap) : x;
+}
+
+struct CacheView {
+    const void *k, *km, *v, *vm;  // plain: k and v; 4-bit: codes and (s, z) pairs
+};
+
+// Partial results of a decode step in its workspace: per split and query head the weighted values [d], the reference and the
+// sum of the softmax; then, for the weights, the scores of every (query head, token) in units of log2 e.
+struct DecWs {
+    float *part, *ml, *scores;  // scores: null if no weights are wanted
+    long long ldt;              // floats between the scores of two heads
+};
+inline size_t dec_ws_bytes(int nsplit, int Hq, int d, long long ldt, bool weights) {
+    return align_up((size_t)nsplit * Hq * (d + 2) * sizeof(float), 256) + (weights ? (size_t)Hq * ldt * sizeof(float) : 0);
+}
+inline long long dec_ldt(int T) { return ((long long)T + 63) / 64 * 64; }
+
+struct DecCall {
+    const void *q;
+    CacheView c;
+    void *o;
+    int T, Hq, Hkv, d;
+    ScoreMod mod;
+    const float *w_in;
+    float *w_out;
+    strd_dtype io;
+    bool kv4;
+};
+
+int dec_splits_general(int T, int Hq, int Hkv, int &tps);
+int dec_combine(const DecCall &a, const DecWs &ws, int nsplit, hipStream_t st);
+
+}  // namespace strd

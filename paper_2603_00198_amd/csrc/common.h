@@ -327,6 +327,18 @@ int ssd_mfma(const void *x, const float *dt, const float *A, const void *B, cons
              const float *S_in, void *y, float *S_out, const int32_t *idx, int N, int K, int T, int H, int P, int G,
              int n, hipStream_t st);
 
+struct AttnMod;  // attn_varlen.h
+bool attn_varlen_mfma_supported(int Hq, int Hkv, int d, strd_dtype io);
+int attn_varlen_general(const void *q, const void *k, const void *v, void *o, int Hq, int Hkv, int d, const AttnMod &mod, long long units,
+                        strd_dtype io, hipStream_t st);
+int kv4_store_launch(const void *k, long long ldk, const void *v, long long ldv, const strd_kv4 &c, int row0, int R, int Hkv, int d,
+                     strd_dtype io, hipStream_t st);
+int kv4_load_launch(const strd_kv4 &c, int row0, int R, void *k, void *v, int Hkv, int d, strd_dtype io, hipStream_t st);
+struct DecCall;  // attn_decode_cache.h
+size_t attn_decode_cache_ws(int T, int Hq, int Hkv, int d, bool kv4, bool weights, strd_dtype io);
+int attn_decode_cache(const DecCall &a, void *ws, hipStream_t st);
+int select_kept_launch(const float *scores, int T, int K, int first, int last, int32_t *idx, void *ws, hipStream_t s);
+
 int mfma_rate_probe(float *out, int workgroups, int iters, int mode, hipStream_t st);
 bool attn_general_supported(int d);
 int attn_general(const void *q, const void *k, const void *v, void *o, int T, int Hq, int Hkv, int d,

@@ -15,7 +15,7 @@
 // loads are in flight and how many workgroups share the work, not by bandwidth.
 #include <algorithm>
 
-#include "common.h"
+#include "attn_varlen.h"
 
 namespace strd {
 namespace {
@@ -807,6 +807,7 @@ __global__ __launch_bounds__(kRecThreads) void ssd_recurrence_kernel(
 }
 
 // ------------------------------------------------------------------ attention --------------
+struct NoMod {};
 // One workgroup per (16 query rows, query head), longest rows first; its NW waves take the key trips in
 // turn, each with an online softmax of its own, and merge through LDS.  S^T = K Q^T keeps the queries
 // on accumulator columns, so the probabilities of a tile are the operand of O^T += V^T P^T as they
@@ -816,19 +817,44 @@ __global__ __launch_bounds__(kRecThreads) void ssd_recurrence_kernel(
 // alone 30 (16 KB per trip and wave from L2, the rate of a CU's path).  Four waves per SIMD overlap the
 // two; a register set for the next trip in two waves per SIMD, two query tiles a wave (half the loads, but
 // too few workgroups for the causal sweep to balance) and 4 or 16 waves were not faster.
-template <typename T, bool VEC, bool FULL, int DJ, int NW, bool WIDE>
+// MOD = AttnMod: a packed batch (one sequence per workgroup, rows with a pitch), scores with a cap and a bias, and vision rows
+// that may see every vision row.  A query then sees the keys before its limit, which never falls from one row to the next.
+template <typename T, bool VEC, bool FULL, int DJ, int NW, bool WIDE, class MOD = NoMod>
 __global__ __launch_bounds__(NW *kWave) __attribute__((amdgpu_waves_per_eu(DJ == 1 ? 4 : 1))) void attn_tile_kernel(
     const T *__restrict__ q, const T *__restrict__ k, const T *__restrict__ v, T *__restrict__ o, int Tn, int Hq, int Hkv,
-    int d, float scale2) {
+    int d, float scale2, MOD mod) {
+    constexpr bool kMod = std::is_same<MOD, AttnMod>::value;
     constexpr int KJ = VEC ? 4 * DJ : 0, KT = DJ == 4 ? 1 : 2, kPitch = 64 * DJ + 4;
     __shared__ __attribute__((aligned(16))) float so[NW][16][kPitch];
     __shared__ float sm[NW][16], sl[NW][16];
     const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lb = lane >> 4, w = wave_index();
-    const int nqt = (Tn + 15) / 16;
-    const int q0 = (nqt - 1 - (int)(blockIdx.x / Hq)) * 16, h = blockIdx.x % Hq, hk = h / (Hq / Hkv);
-    const int ntrip = (min(Tn, q0 + 16) + 16 * KT - 1) / (16 * KT);
+    const int nqt = (Tn + 15) / 16, h = blockIdx.x % Hq, hk = h / (Hq / Hkv);
+    int q0 = (nqt - 1 - (int)(blockIdx.x / Hq)) * 16;
+    size_t ldq = (size_t)Hq * d, ldk = (size_t)Hkv * d, ldv = ldk;
+    int lim_lo = q0 + 1, lim_hi = min(Tn, q0 + 16), lim = 0;  // keys of the block's first query, of all of it, of this lane's query
+    float slope = 0.f, pos_t = 0.f;
+    const int32_t *pos = nullptr;
+    if constexpr (kMod) {
+        int level, s;
+        mod.tab.locate(blockIdx.x / Hq, level, s);
+        q0 = 16 * level;
+        Tn = mod.tab.len[s];
+        const int vis = mod.prefix ? mod.tab.vis[s] : 0;
+        const size_t row0 = (size_t)mod.tab.row0[s];
+        ldq = mod.ldq, ldk = mod.ldk, ldv = mod.ldv;
+        q += row0 * ldq, k += row0 * ldk, v += row0 * ldv, o += row0 * Hq * d;
+        lim = min(max(q0 + lr + 1, q0 + lr < vis ? vis : 0), Tn);
+        lim_lo = q0 < vis ? vis : q0 + 1;
+        lim_hi = max(min(Tn, q0 + 16), q0 < vis ? vis : 0);
+        if (mod.slopes) {
+            slope = mod.slopes[h];
+            if (mod.pos) pos = mod.pos + row0;
+            pos_t = pos ? (float)pos[min(q0 + lr, Tn - 1)] : (float)(q0 + lr);
+        }
+    }
+    const int ntrip = (lim_hi + 16 * KT - 1) / (16 * KT);
     Operand<T, KJ, FULL> qf;
-    qf.load(q + ((size_t)min(q0 + lr, Tn - 1) * Hq + h) * d, lb, d);
+    qf.load(q + (size_t)min(q0 + lr, Tn - 1) * ldq + (size_t)h * d, lb, d);
     f32x4 acc[DJ][4];
 #pragma unroll
     for (int b = 0; b < DJ; ++b)
@@ -838,22 +864,21 @@ __global__ __launch_bounds__(NW *kWave) __attribute__((amdgpu_waves_per_eu(DJ ==
     // Rows of a trip: one address per workgroup and trip plus a 24-bit product per row (they lie within 32
     // rows of each other; WIDE, for rows of 16 MB and more: a full product); rows past the end of the sequence
     // re-read its last one.
-    const size_t stride = (size_t)Hkv * d * sizeof(T);
-    auto row_of = [&](const T *base, int r, int last) {
-        const size_t off = WIDE ? (unsigned)min(r, last) * stride : __umul24((unsigned)min(r, last), (unsigned)stride);
+    auto row_of = [&](const T *base, size_t ld, int r, int last) {
+        const size_t off = WIDE ? (unsigned)min(r, last) * (ld * sizeof(T)) : __umul24((unsigned)min(r, last), (unsigned)(ld * sizeof(T)));
         return reinterpret_cast<const T *>(reinterpret_cast<const char *>(base) + off);
     };
     auto body = [&](auto edge, int trip) __attribute__((always_inline)) {
         const int key0 = trip * KT * 16, last = Tn - 1 - key0;  // uniform
-        const T *kb = k + ((size_t)key0 * Hkv + hk) * d, *vb = v + ((size_t)key0 * Hkv + hk) * d;
+        const T *kb = k + (size_t)key0 * ldk + (size_t)hk * d, *vb = v + (size_t)key0 * ldv + (size_t)hk * d;
         Operand<T, KJ, FULL> kf[KT];
         float vf[KT][4][DJ][4];
 #pragma unroll
         for (int u = 0; u < KT; ++u) {
-            kf[u].load(row_of(kb, 16 * u + lr, last), lb, d);
+            kf[u].load(row_of(kb, ldk, 16 * u + lr, last), lb, d);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const T *vr = row_of(vb, 16 * u + 4 * lb + i, last);
+                const T *vr = row_of(vb, ldv, 16 * u + 4 * lb + i, last);
 #pragma unroll
                 for (int b = 0; b < DJ; ++b) {
                     if constexpr (VEC) {
@@ -877,7 +902,15 @@ __global__ __launch_bounds__(NW *kWave) __attribute__((amdgpu_waves_per_eu(DJ ==
         for (int u = 0; u < KT; ++u)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                if (key0 + 16 * u + 4 * lb + i > q0 + lr) z[u][i] = -INFINITY;
+                const int key = key0 + 16 * u + 4 * lb + i;
+                if constexpr (kMod) {  // in units of log2 e from here on (scale2 is 1)
+                    float x = z[u][i] * mod.scale;
+                    if (mod.cap > 0.f) x = mod.cap * tanhf(x * mod.inv_cap);  // tanhf: the scores' errors are the weights' relative errors
+                    if (mod.slopes) x -= slope * fabsf(pos_t - (pos ? (float)pos[min(key, Tn - 1)] : (float)key));
+                    z[u][i] = key >= lim ? -INFINITY : x * kLog2e;
+                } else if (key > q0 + lr) {
+                    z[u][i] = -INFINITY;
+                }
                 tmax = fmaxf(tmax, z[u][i]);
             }
         // (a trip starts at or before the block's first query: every query sees a key of every trip)
@@ -907,6 +940,15 @@ __global__ __launch_bounds__(NW *kWave) __attribute__((amdgpu_waves_per_eu(DJ ==
 #pragma unroll
             for (int u = 0; u < KT; ++u) {
                 const int ahead = key0 + 16 * u - q0;
+                if constexpr (kMod) {  // keys that no query of the block sees; then the one tile of which some see more than others
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int b = 0; b < DJ; ++b)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) vf[u][i][b][e] = key0 + 16 * u + 4 * lb + i < lim_hi ? vf[u][i][b][e] : 0.f;
+                    if (ahead != 0 || lim_lo >= lim_hi) continue;
+                }
                 if (ahead < 0) continue;
                 float t = 0.f;
 #pragma unroll
@@ -940,8 +982,8 @@ __global__ __launch_bounds__(NW *kWave) __attribute__((amdgpu_waves_per_eu(DJ ==
             for (int s = 0; s < 16; ++s) {
                 const float mine = s & 2 ? (s & 1 ? zd[3] : zd[2]) : (s & 1 ? zd[1] : zd[0]);
                 const float pr = __shfl(mine, 16 * (s >> 2) + lr, kWave);
-                const T *vr = row_of(vb, first + s, last);
-                if (s > lr) continue;
+                const T *vr = row_of(vb, ldv, first + s, last);
+                if (kMod ? key0 + first + s >= lim : s > lr) continue;
 #pragma unroll
                 for (int b = 0; b < DJ; ++b)
 #pragma unroll
@@ -1357,7 +1399,7 @@ static int attn_launch(const void *q, const void *k, const void *v, void *o, int
     const bool wide = (long long)Hkv * d * (long long)sizeof(T) >= 1 << 24;  // rows that a 24-bit product does not reach
 #define STRD_ATTN_W(VV, FF, DD, NN, WW)                                                                                  \
     attn_tile_kernel<T, VV, FF, DD, NN, WW><<<(unsigned)grid, NN * kWave, 0, st>>>(                                      \
-        (const T *)q, (const T *)k, (const T *)v, (T *)o, Tn, Hq, Hkv, d, scale * kLog2e)
+        (const T *)q, (const T *)k, (const T *)v, (T *)o, Tn, Hq, Hkv, d, scale * kLog2e, NoMod())
 #define STRD_ATTN(VV, FF, DD, NN) STRD_ATTN_W(VV, FF, DD, NN, false)
     if (wide) {
         if (d <= 64) STRD_ATTN_W(false, false, 1, 8, true);
@@ -1376,6 +1418,40 @@ static int attn_launch(const void *q, const void *k, const void *v, void *o, int
 #undef STRD_ATTN
 #undef STRD_ATTN_W
     return launch_status();
+}
+
+// Packed batches with capped and biased scores: the tiles, whatever the length (rows of long sequences and of short ones
+// share a launch).
+template <typename T>
+static int attn_mod_launch(const void *q, const void *k, const void *v, void *o, int Hq, int Hkv, int d, const AttnMod &mod, long long units,
+                           hipStream_t st) {
+    const long long grid = units * Hq;
+    if (grid > 0x7FFFFFFFLL) return STRD_EUNSUPPORTED;
+    const bool wide = std::max(mod.ldk, mod.ldv) * (long long)sizeof(T) >= 1 << 24;
+    const bool vec = vec4<T>(d, (const T *)q, (const T *)k, (const T *)v) && mod.ldq % 4 == 0 && mod.ldk % 4 == 0 && mod.ldv % 4 == 0 && !wide;
+#define STRD_ATTN_M(VV, FF, DD, NN, WW)                                                                                    \
+    attn_tile_kernel<T, VV, FF, DD, NN, WW, AttnMod><<<(unsigned)grid, NN * kWave, 0, st>>>(                               \
+        (const T *)q, (const T *)k, (const T *)v, (T *)o, 0, Hq, Hkv, d, 1.f, mod)
+    if (d <= 64) {
+        if (!vec) STRD_ATTN_M(false, false, 1, 8, true);
+        else if (d == 64) STRD_ATTN_M(true, true, 1, 8, false);
+        else STRD_ATTN_M(true, false, 1, 8, false);
+    } else if (d <= 128) {
+        if (!vec) STRD_ATTN_M(false, false, 2, 4, true);
+        else if (d == 128) STRD_ATTN_M(true, true, 2, 4, false);
+        else STRD_ATTN_M(true, false, 2, 4, false);
+    } else {
+        if (!vec) STRD_ATTN_M(false, false, 4, 2, true);
+        else STRD_ATTN_M(true, false, 4, 2, false);
+    }
+#undef STRD_ATTN_M
+    return launch_status();
+}
+
+int attn_varlen_general(const void *q, const void *k, const void *v, void *o, int Hq, int Hkv, int d, const AttnMod &mod, long long units,
+                        strd_dtype io, hipStream_t st) {
+    if (io == STRD_F32) return attn_mod_launch<float>(q, k, v, o, Hq, Hkv, d, mod, units, st);
+    return attn_mod_launch<bf16_t>(q, k, v, o, Hq, Hkv, d, mod, units, st);
 }
 
 int attn_general(const void *q, const void *k, const void *v, void *o, int T, int Hq, int Hkv, int d,

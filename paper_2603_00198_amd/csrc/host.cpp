@@ -11,9 +11,11 @@
 #include <Python.h>
 // (torch's headers need Python.h first)
 #include <ATen/hip/EmptyTensor.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPCachingAllocator.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -508,6 +510,225 @@ PyObject *attn_decode_step(Args a) {  // q, k_cache, v_cache, scale, ws
     return wrap(std::move(o));
 }
 
+// ------------------------------------------------------------------ packed attention, caches -
+// The calls of this part run on their tensors' device, whatever the current one is, on its current stream.
+struct On {
+    const Tensor &like;
+    c10::OptionalDeviceGuard guard;
+    hipStream_t st;
+    explicit On(const Tensor &t) : like(t), guard(t.device()), st(c10::hip::getCurrentHIPStream(t.device().index()).stream()) {}
+    const On &with(const Tensor &t) const {
+        if (t.device() != like.device()) fail("tensors must live on one device");
+        return *this;
+    }
+    const On &with(const Tensor *t) const { return t ? with(*t) : *this; }
+};
+
+// Elements between the rows of a [rows, H, d] tensor whose rows are contiguous (a column range of a projection is fine).
+int64_t row_pitch(const Tensor &t, const char *what) {
+    if (!t.is_cuda()) fail("tensors must live on the GPU");
+    if (t.dim() != 3) fail(std::string(what) + ": a tensor [rows, heads, d] is needed");
+    const int64_t own = t.size(1) * t.size(2);
+    if (t.numel() == 0) return own;
+    if ((t.size(2) > 1 && t.stride(2) != 1) || (t.size(1) > 1 && t.stride(1) != t.size(2)) || (t.size(0) > 1 && t.stride(0) < own))
+        fail(std::string(what) + ": heads and channels of a row must be contiguous, rows apart");
+    return t.size(0) > 1 ? t.stride(0) : own;
+}
+
+// slopes [Hq] fp32 and positions [rows] int32, or None
+struct Bias {
+    const Tensor *slopes, *pos;
+    Bias(PyObject *s, PyObject *p, int64_t Hq, int64_t rows, const On &on, const char *what) : slopes(opt(s)), pos(opt(p)) {
+        if (slopes && (slopes->dim() != 1 || slopes->size(0) != Hq || !is_f32(*slopes))) fail(std::string(what) + ": slopes must be fp32 [Hq]");
+        if (pos && (pos->dim() != 1 || pos->size(0) < rows || pos->scalar_type() != at::kInt)) fail(std::string(what) + ": pos must be int32, one per row");
+        on.with(slopes).with(pos);
+    }
+};
+
+PyObject *attn_prefill_varlen(Args a) {  // q, k, v, seqs, prefix, cap, slopes, pos, scale, out
+    const Tensor &q = tensor(a[0]), &k = tensor(a[1]), &v = tensor(a[2]);
+    const int64_t ldq = row_pitch(q, "q"), ldk = row_pitch(k, "k"), ldv = row_pitch(v, "v");
+    const Seqs sq(a[3]);
+    if (k.size(0) != q.size(0) || k.size(2) != q.size(2) || v.sizes() != k.sizes() || k.scalar_type() != q.scalar_type() ||
+        v.scalar_type() != q.scalar_type() || q.size(0) != sq.rows)
+        fail("attn_prefill_varlen: q/k/v/seqs mismatch");
+    const On on(q);
+    on.with(k).with(v);
+    const strd_dtype io = io_of(q);
+    const int Hq = size(q, 1), d = size(q, 2), Hkv = size(k, 1), prefix = truth(a[4]);
+    const float cap = (float)number(a[5]), scale = scale_or_default(a[8], d);
+    const Bias b(a[6], a[7], Hq, sq.rows, on, "attn_prefill_varlen");
+    Tensor o = out_or(a[9], q.sizes(), q.scalar_type(), q);
+    if (o.sizes() != q.sizes() || o.scalar_type() != q.scalar_type()) fail("attn_prefill_varlen: out must be as q");
+    on.with(o);
+    check(call([&] {
+              return strd_attn_prefill_varlen(q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, o.data_ptr(), sq.s, sq.n, prefix, cap,
+                                              f32(b.slopes), i32(b.pos), Hq, Hkv, d, scale, io, on.st);
+          }),
+          "attn_prefill_varlen");
+    return wrap(std::move(o));
+}
+
+// The four tensors of a 4-bit cache.
+struct Kv4 {
+    Tensor t[4];
+    strd_kv4 c;
+    int rows = 0, Hkv = 0, d = 0;
+    Kv4(PyObject *o, const char *what) {
+        Sequence s(o);
+        bool ok = s.size() == 4;
+        for (int i = 0; ok && i < 4; ++i) t[i] = dev(s[i]);
+        for (int i = 0; ok && i < 4; i += 2)
+            ok = t[i].dim() == 3 && t[i].scalar_type() == at::kByte && t[i + 1].dim() == 4 && t[i + 1].scalar_type() == at::kBFloat16 &&
+                 t[i].sizes() == t[0].sizes() && t[i + 1].size(0) == t[0].size(0) && t[i + 1].size(1) == t[0].size(1) &&
+                 t[i + 1].size(2) * 16 == t[0].size(2) && t[i + 1].size(3) == 2 && t[i].device() == t[0].device() && t[i + 1].device() == t[0].device();
+        if (!ok) fail(std::string(what) + ": a cache is (k_codes, k_meta, v_codes, v_meta): uint8 [rows, Hkv, d/2], bf16 [rows, Hkv, d/32, 2]");
+        rows = size(t[0], 0), Hkv = size(t[0], 1), d = narrow(2 * t[0].size(2), "d");
+        c = {t[0].data_ptr(), t[1].data_ptr(), t[2].data_ptr(), t[3].data_ptr()};
+    }
+};
+
+PyObject *kv4_store(Args a) {  // k, v, cache, row0
+    const Tensor &k = tensor(a[0]), &v = tensor(a[1]);
+    const int64_t ldk = row_pitch(k, "k"), ldv = row_pitch(v, "v");
+    const Kv4 c(a[2], "kv4_store");
+    const int row0 = integer(a[3], "row0");
+    if (v.sizes() != k.sizes() || v.scalar_type() != k.scalar_type() || k.size(1) != c.Hkv || k.size(2) != c.d)
+        fail("kv4_store: k, v [R, Hkv, d] of one dtype, as the cache's rows");
+    const strd_dtype io = io_of(k);
+    const int R = size(k, 0);
+    const On on(k);
+    on.with(v).with(c.t[0]);
+    check(call([&] { return strd_kv4_store(k.data_ptr(), ldk, v.data_ptr(), ldv, &c.c, c.rows, row0, R, c.Hkv, c.d, io, on.st); }), "kv4_store");
+    return none();
+}
+
+PyObject *kv4_load(Args a) {  // cache, row0, R, dtype
+    const Kv4 c(a[0], "kv4_load");
+    const int row0 = integer(a[1], "row0"), R = integer(a[2], "R");
+    if (!THPDtype_Check(a[3])) fail("kv4_load: a torch dtype is needed");
+    const at::ScalarType type = reinterpret_cast<THPDtype *>(a[3])->scalar_type;
+    if (type != at::kFloat && type != at::kBFloat16) fail("kv4_load: fp32 or bf16");
+    if (R < 0 || row0 < 0 || (int64_t)row0 + R > c.rows) fail("kv4_load: rows outside the cache");
+    const On on(c.t[0]);
+    Tensor k = empty({R, c.Hkv, c.d}, type, c.t[0]), v = empty({R, c.Hkv, c.d}, type, c.t[0]);
+    check(call([&] {
+              return strd_kv4_load(&c.c, c.rows, row0, R, k.data_ptr(), v.data_ptr(), c.Hkv, c.d, type == at::kFloat ? STRD_F32 : STRD_BF16, on.st);
+          }),
+          "kv4_load");
+    return pair(wrap(std::move(k)), wrap(std::move(v)));
+}
+
+// What the two decode steps share: weights [>= T] fp32 or None in, a tensor or a new one out (or none).
+struct Weights {
+    const Tensor *in;
+    Tensor out;
+    Weights(PyObject *w, PyObject *given, bool want, int T, const On &on, const char *what) : in(opt(w)) {
+        if (!want && (in || given != Py_None)) fail(std::string(what) + ": weights given, none wanted");
+        if (want) out = out_or(given, {T}, at::kFloat, on.like);
+        const Tensor *both[2] = {in, want ? &out : nullptr};
+        for (const Tensor *t : both)
+            if (t && (t->dim() != 1 || t->size(0) < T || !is_f32(*t))) fail(std::string(what) + ": weights must be fp32 [T]");
+        on.with(in);
+        if (want) on.with(out);
+    }
+    float *p() { return out.defined() ? f32(&out) : nullptr; }
+    PyObject *py() { return out.defined() ? wrap(std::move(out)) : none(); }
+};
+
+PyObject *attn_decode_step_kv4(Args a) {  // q, cache, T, scale, cap, slopes, pos, weights, weights_out, want_weights, ws
+    const Tensor &q = dev(a[0]);
+    const Kv4 c(a[1], "attn_decode_step_kv4");
+    const int T = integer(a[2], "T");
+    if (q.dim() != 2 || q.size(1) != c.d || T < 1 || T > c.rows) fail("attn_decode_step_kv4: q [Hq, d], 1 <= T <= the cache's rows");
+    const On on(q);
+    on.with(c.t[0]);
+    const strd_dtype io = io_of(q);
+    const int Hq = size(q, 0), d = c.d;
+    const float scale = scale_or_default(a[3], d), cap = (float)number(a[4]);
+    const Bias b(a[5], a[6], Hq, T, on, "attn_decode_step_kv4");
+    Weights w(a[7], a[8], truth(a[9]), T, on, "attn_decode_step_kv4");
+    Tensor o = empty(q.sizes(), q.scalar_type(), q);
+    Workspace ws(a[10], a[10] == Py_None ? strd_attn_decode_step_kv4_workspace(T, Hq, c.Hkv, d, w.p() != nullptr, io) : 0, q, on.st);
+    check(call([&] {
+              return strd_attn_decode_step_kv4(q.data_ptr(), &c.c, o.data_ptr(), T, Hq, c.Hkv, d, scale, cap, f32(b.slopes), i32(b.pos), f32(w.in),
+                                               w.p(), io, ws.p, ws.bytes, on.st);
+          }),
+          "attn_decode_step_kv4");
+    return pair(wrap(std::move(o)), w.py());
+}
+
+PyObject *attn_decode_step_weights(Args a) {  // q, k_cache, v_cache, scale, cap, slopes, pos, weights, weights_out, want_weights, ws
+    const Tensor &q = dev(a[0]), &k = dev(a[1]), &v = dev(a[2]);
+    if (q.dim() != 2 || k.dim() != 3 || k.size(2) != q.size(1) || v.sizes() != k.sizes() || k.scalar_type() != q.scalar_type() ||
+        v.scalar_type() != q.scalar_type())
+        fail("attn_decode_step_weights: inconsistent shapes or dtypes");
+    const On on(q);
+    on.with(k).with(v);
+    const strd_dtype io = io_of(q);
+    const int Hq = size(q, 0), d = size(q, 1), T = size(k, 0), Hkv = size(k, 1);
+    const float scale = scale_or_default(a[3], d), cap = (float)number(a[4]);
+    const Bias b(a[5], a[6], Hq, T, on, "attn_decode_step_weights");
+    Weights w(a[7], a[8], truth(a[9]), T, on, "attn_decode_step_weights");
+    Tensor o = empty(q.sizes(), q.scalar_type(), q);
+    Workspace ws(a[10], a[10] == Py_None ? strd_attn_decode_step_weights_workspace(T, Hq, Hkv, d, w.p() != nullptr, io) : 0, q, on.st);
+    check(call([&] {
+              return strd_attn_decode_step_weights(q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), T, Hq, Hkv, d, scale, cap,
+                                                   f32(b.slopes), i32(b.pos), f32(w.in), w.p(), io, ws.p, ws.bytes, on.st);
+          }),
+          "attn_decode_step_weights");
+    return pair(wrap(std::move(o)), w.py());
+}
+
+PyObject *cache_evict(Args a) {  // weights, K, first, last, tensors, pos, outs, ws
+    const Tensor &w = dev(a[0]);
+    if (!is_f32(w) || w.dim() != 1) fail("cache_evict: weights must be fp32 [T]");
+    const int T = size(w, 0), K = integer(a[1], "K"), first = integer(a[2], "first"), last = integer(a[3], "last");
+    if (K < 1 || K > T || first < 0 || last < 0 || (int64_t)first + last > K)
+        fail("cache_evict: 1 <= K <= T, first + last <= K");
+    Sequence list(a[4]);
+    const int n = (int)list.size();
+    if (list.size() > STRD_COMPACT_MAX - 1) fail("cache_evict: too many tensors: " + std::string(strd_status_string(STRD_EINVAL)));
+    const Tensor *pos = opt(a[5]);
+    if (pos && (pos->dim() != 1 || pos->size(0) != T || pos->scalar_type() != at::kInt)) fail("cache_evict: pos must be int32 [T]");
+    const On on(w);
+    on.with(pos);
+    strd_compact_item items[STRD_COMPACT_MAX];
+    Tensor dst[STRD_COMPACT_MAX];
+    if (a[6] != Py_None) {
+        Sequence outs(a[6]);
+        if (outs.size() != n) fail("cache_evict: one output per tensor");
+        for (int i = 0; i < n; ++i) dst[i] = dev(outs[i]);
+    }
+    for (int i = 0; i < n; ++i) {
+        const Tensor &t = dev(list[i]);
+        const Sizes sz(K, t);
+        if (a[6] == Py_None) dst[i] = empty(sz, t.scalar_type(), t);
+        if (t.size(0) != T || dst[i].scalar_type() != t.scalar_type() || dst[i].sizes() != at::IntArrayRef(sz))
+            fail("cache_evict: tensor " + std::to_string(i) + " has the wrong shape");
+        on.with(t).with(dst[i]);
+        items[i] = {t.data_ptr(), dst[i].data_ptr(), sz.row() * (int64_t)t.element_size()};
+    }
+    Tensor idx = empty({K}, at::kInt, w), kept = empty({K}, at::kFloat, w), pos_out;
+    if (pos) pos_out = empty({K}, at::kInt, w);
+    Workspace ws(a[7], a[7] == Py_None ? strd_cache_evict_workspace(T, K, first, last) : 0, w, on.st);
+    check(call([&] {
+              return strd_cache_evict(f32(w), T, K, first, last, items, n, i32(pos), pos ? (int32_t *)pos_out.data_ptr() : nullptr,
+                                      (int32_t *)idx.data_ptr(), f32(&kept), ws.p, ws.bytes, on.st);
+          }),
+          "cache_evict");
+    PyObject *rows = a[6] == Py_None ? PyList_New(n) : PySequence_List(a[6]);
+    if (!rows) throw python_error();
+    if (a[6] == Py_None)
+        for (int i = 0; i < n; ++i) PyList_SET_ITEM(rows, i, wrap(std::move(dst[i])));
+    PyObject *r = PyTuple_New(4);
+    PyTuple_SET_ITEM(r, 0, wrap(std::move(idx)));
+    PyTuple_SET_ITEM(r, 1, wrap(std::move(kept)));
+    PyTuple_SET_ITEM(r, 2, rows);
+    PyTuple_SET_ITEM(r, 3, pos ? wrap(std::move(pos_out)) : none());
+    return r;
+}
+
 // ------------------------------------------------------------------ block glue -------------
 // Row pitch in elements of a 2-D GPU tensor whose rows are contiguous (a column slice is fine).
 int pitch(const Tensor &t, const char *what) {
@@ -612,7 +833,8 @@ PyMethodDef methods[] = {
     STRD_ENTRY(score_attn_varlen), STRD_ENTRY(score_mamba_varlen), STRD_ENTRY(select_topk_varlen), STRD_ENTRY(compact_varlen),
     STRD_ENTRY(ssd_prefill), STRD_ENTRY(ssd_prefill_gather), STRD_ENTRY(attn_prefill), STRD_ENTRY(ssd_decode_step),
     STRD_ENTRY(attn_decode_step), STRD_ENTRY(linear), STRD_ENTRY(rmsnorm), STRD_ENTRY(gated_rmsnorm), STRD_ENTRY(conv1d_silu),
-    STRD_ENTRY(softplus_dt), {nullptr, nullptr, 0, nullptr}};
+    STRD_ENTRY(softplus_dt), STRD_ENTRY(attn_prefill_varlen), STRD_ENTRY(kv4_store), STRD_ENTRY(kv4_load), STRD_ENTRY(attn_decode_step_kv4),
+    STRD_ENTRY(attn_decode_step_weights), STRD_ENTRY(cache_evict), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "strd_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -50,7 +50,19 @@ __device__ __forceinline__ uint32_t order_key(float f) {
     return max((b & 0x80000000u) ? ~b : (b | 0x80000000u), 1u);
 }
 
-// Keys of the 4 scores this lane owns in tile `t` (0 past the end).
+// A selection that leaves out the first rows, which are kept whatever they score, and those from N on (cache_evict): their
+// slots have key 0 as those past the end, and one workgroup writes their indices around the selected ones.  K and idx are the
+// selection's, idx + K the place of the last rows.
+struct Kept {
+    int first, last;
+};
+template <class SEQ> constexpr bool is_kept() { return std::is_same<SEQ, Kept>::value; }
+__device__ __forceinline__ void write_kept(const Kept &kept, int N, int K, int32_t *__restrict__ idx) {
+    for (int i = threadIdx.x; i < kept.first; i += kThreads) idx[i - kept.first] = i;
+    for (int i = threadIdx.x; i < kept.last; i += kThreads) idx[K + i] = N + i;
+}
+
+// Keys of the 4 scores this lane owns in tile `t` (0 past the end and, of a Kept selection, before its first row).
 __device__ __forceinline__ void load_tile(const float *__restrict__ scores, int N, int t, uint32_t (&key)[4]) {
     const int i0 = t * kTile + threadIdx.x * 4;
     if (i0 + 3 < N) {
@@ -59,6 +71,15 @@ __device__ __forceinline__ void load_tile(const float *__restrict__ scores, int 
     } else {
 #pragma unroll
         for (int u = 0; u < 4; ++u) key[u] = (i0 + u < N) ? order_key(scores[i0 + u]) : 0u;
+    }
+}
+template <class SEQ>
+__device__ __forceinline__ void load_tile(const float *__restrict__ scores, int N, int t, uint32_t (&key)[4], const SEQ &seq) {
+    load_tile(scores, N, t, key);
+    if constexpr (is_kept<SEQ>()) {
+        const int i0 = t * kTile + threadIdx.x * 4;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) key[u] = i0 + u < seq.first ? 0u : key[u];
     }
 }
 
@@ -221,6 +242,7 @@ __global__ __launch_bounds__(kThreads) void select_topk_kernel(const float *__re
         scores += (size_t)b * ld;
         idx += seq.koff[b];
     }
+    if constexpr (is_kept<SEQ>()) write_kept(seq, N, K, idx);
     constexpr int kCop = kCopies<TILES>;
     extern __shared__ __attribute__((aligned(16))) uint32_t hist[];  // [kBins][kCop]
     __shared__ ScanScratch scan[2];          // taken in turn by the batches of the write-out
@@ -241,7 +263,7 @@ __global__ __launch_bounds__(kThreads) void select_topk_kernel(const float *__re
     uint32_t held[kHeld][4];
     if (TILES > 0) {
 #pragma unroll
-        for (int t = 0; t < kHeld; ++t) load_tile(scores, N, t, held[t]);
+        for (int t = 0; t < kHeld; ++t) load_tile(scores, N, t, held[t], seq);
     }
     // Visit every key this lane owns; f is inlined into both variants.
     auto for_each_key = [&](auto &&f) {
@@ -254,7 +276,7 @@ __global__ __launch_bounds__(kThreads) void select_topk_kernel(const float *__re
             for (int t0 = 0; t0 < ntiles; t0 += kBatch) {
                 uint32_t key[kBatch][4];
 #pragma unroll
-                for (int b = 0; b < kBatch; ++b) load_tile(scores, N, t0 + b, key[b]);  // past-the-end tiles give 0
+                for (int b = 0; b < kBatch; ++b) load_tile(scores, N, t0 + b, key[b], seq);  // past-the-end tiles give 0
 #pragma unroll
                 for (int b = 0; b < kBatch; ++b)
 #pragma unroll
@@ -384,7 +406,7 @@ __global__ __launch_bounds__(kThreads) void select_topk_kernel(const float *__re
         for (int t0 = 0; t0 < ntiles; t0 += kHold) {
             uint32_t key[kHold][4];
 #pragma unroll
-            for (int b = 0; b < kHold; ++b) load_tile(scores, N, t0 + b, key[b]);
+            for (int b = 0; b < kHold; ++b) load_tile(scores, N, t0 + b, key[b], seq);
             emit_batch(t0, key, scan[(t0 / kHold) & 1]);
         }
     }
@@ -435,10 +457,11 @@ struct WideWs {
     uint16_t from[kWideMax][kLastBins];  // per tile, two digits picked: keys in the bin whose low bits are at least so much
 };
 
-__global__ __launch_bounds__(kThreads) void topk_wide_range_kernel(const float *__restrict__ scores, int N, WideWs *ws) {
+template <class SEQ>
+__global__ __launch_bounds__(kThreads) void topk_wide_range_kernel(const float *__restrict__ scores, int N, WideWs *ws, SEQ seq) {
     __shared__ uint32_t buf[2][kWaves];
     uint32_t key[4];
-    load_tile(scores, N, blockIdx.x, key);
+    load_tile(scores, N, blockIdx.x, key, seq);
     for (int i = blockIdx.x * kThreads + threadIdx.x; i < 3 * kBins; i += gridDim.x * kThreads) ws->ghist[i / kBins][i % kBins] = 0u;
     if (blockIdx.x == 0 && threadIdx.x == 0) ws->ncand = ws->low_inv = ws->low_max = 0u;
     uint32_t kmin = 0xFFFFFFFFu, kmax = 0u;
@@ -467,12 +490,13 @@ __device__ __forceinline__ void wide_range(const WideWs *ws, uint32_t (&buf)[2][
     shift = max(32 - __clz(kmax - kmin) - 11, 0);
 }
 
-__global__ __launch_bounds__(kThreads) void topk_wide_hist_kernel(const float *__restrict__ scores, int N, WideWs *ws) {
+template <class SEQ>
+__global__ __launch_bounds__(kThreads) void topk_wide_hist_kernel(const float *__restrict__ scores, int N, WideWs *ws, SEQ seq) {
     __shared__ __attribute__((aligned(16))) uint32_t hist[kBins * kWideCopies];
     __shared__ uint32_t buf[2][kWaves];
     const int tid = threadIdx.x;
     uint32_t key[4], kmin;
-    load_tile(scores, N, blockIdx.x, key);
+    load_tile(scores, N, blockIdx.x, key, seq);
     for (int b = tid * 4; b < kBins * kWideCopies; b += kThreads * 4)
         *reinterpret_cast<uint4 *>(&hist[b]) = make_uint4(0, 0, 0, 0);
     int shift;
@@ -487,9 +511,9 @@ __global__ __launch_bounds__(kThreads) void topk_wide_hist_kernel(const float *_
     }
 }
 
-template <int PASS>
+template <int PASS, class SEQ>
 __global__ __launch_bounds__(kThreads) void topk_wide_collect_kernel(const float *__restrict__ scores, int N, int K,
-                                                                       WideWs *ws) {
+                                                                       WideWs *ws, SEQ seq) {
     __shared__ __attribute__((aligned(16))) uint32_t hist[kBins * kWideCopies];  // the picked digit's, then the next one's
     __shared__ uint32_t buf[2][kWaves];
     __shared__ ScanScratch scan;
@@ -500,7 +524,7 @@ __global__ __launch_bounds__(kThreads) void topk_wide_collect_kernel(const float
         const uint32_t c = ws->pick[0].count;
         if (c <= (uint32_t)kWideCand || ~ws->low_inv == ws->low_max) return;  // uniform, the same in every workgroup
     }
-    load_tile(scores, N, blockIdx.x, key);
+    load_tile(scores, N, blockIdx.x, key, seq);
     for (int b = tid; b < kBins; b += kThreads) hist[b] = ws->ghist[PASS][b];
     int shift;
     wide_range(ws, buf, kmin, shift);  // its barrier publishes the bins
@@ -584,15 +608,18 @@ __global__ __launch_bounds__(kThreads) void topk_wide_collect_kernel(const float
     }
 }
 
+template <class SEQ>
 __global__ __launch_bounds__(kThreads) void topk_wide_emit_kernel(const float *__restrict__ scores, int N, int K,
                                                                     const WideWs *__restrict__ ws,
-                                                                    int32_t *__restrict__ idx) {
+                                                                    int32_t *__restrict__ idx, SEQ seq) {
     __shared__ __attribute__((aligned(16))) uint32_t hist[kBins * kFewCopies];
     __shared__ ScanScratch scan[2];
     __shared__ uint32_t found[2][3], cand[kRankKeys], ncand, ranked[2];
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
     uint32_t key[4];
-    load_tile(scores, N, blockIdx.x, key);
+    load_tile(scores, N, blockIdx.x, key, seq);
+    if constexpr (is_kept<SEQ>())
+        if (blockIdx.x == 0) write_kept(seq, N, K, idx);
     uint32_t before_gt = 0, before_eq = 0;  // this thread's share of the keys above / in the bin in earlier tiles
     if (tid < (int)blockIdx.x) {
         before_gt = ws->counts[tid][0];
@@ -711,22 +738,41 @@ int select_topk_varlen_launch(const float *scores, int ld, const SeqTab &tab, in
                                 : launch_select<8>(scores, 0, 0, idx, tab, ld, nseq, s);
 }
 
-int select_topk_launch(const float *scores, int N, int K, int32_t *idx, void *ws, hipStream_t s) {
+template <class SEQ>
+static int select_launch(const float *scores, int N, int K, int32_t *idx, void *ws, const SEQ &seq, hipStream_t s) {
     if (select_topk_ws(N)) {
         WideWs *w = reinterpret_cast<WideWs *>(ws);
         const int G = ceil_div(N, kTile);
-        topk_wide_range_kernel<<<G, kThreads, 0, s>>>(scores, N, w);
-        topk_wide_hist_kernel<<<G, kThreads, 0, s>>>(scores, N, w);
-        topk_wide_collect_kernel<0><<<G, kThreads, 0, s>>>(scores, N, K, w);
-        topk_wide_collect_kernel<1><<<G, kThreads, 0, s>>>(scores, N, K, w);
-        topk_wide_emit_kernel<<<G, kThreads, 0, s>>>(scores, N, K, w, idx);
+        topk_wide_range_kernel<<<G, kThreads, 0, s>>>(scores, N, w, seq);
+        topk_wide_hist_kernel<<<G, kThreads, 0, s>>>(scores, N, w, seq);
+        topk_wide_collect_kernel<0><<<G, kThreads, 0, s>>>(scores, N, K, w, seq);
+        topk_wide_collect_kernel<1><<<G, kThreads, 0, s>>>(scores, N, K, w, seq);
+        topk_wide_emit_kernel<<<G, kThreads, 0, s>>>(scores, N, K, w, idx, seq);
         return launch_status();
     }
-    return N <= kTile       ? launch_select<1>(scores, N, K, idx, OneSeq(), 0, 1, s)
-           : N <= 2 * kTile ? launch_select<2>(scores, N, K, idx, OneSeq(), 0, 1, s)
-           : N <= 4 * kTile ? launch_select<4>(scores, N, K, idx, OneSeq(), 0, 1, s)
-           : N <= 8 * kTile ? launch_select<8>(scores, N, K, idx, OneSeq(), 0, 1, s)
-                            : launch_select<0>(scores, N, K, idx, OneSeq(), 0, 1, s);
+    return N <= kTile       ? launch_select<1>(scores, N, K, idx, seq, 0, 1, s)
+           : N <= 2 * kTile ? launch_select<2>(scores, N, K, idx, seq, 0, 1, s)
+           : N <= 4 * kTile ? launch_select<4>(scores, N, K, idx, seq, 0, 1, s)
+           : N <= 8 * kTile ? launch_select<8>(scores, N, K, idx, seq, 0, 1, s)
+                            : launch_select<0>(scores, N, K, idx, seq, 0, 1, s);
+}
+
+int select_topk_launch(const float *scores, int N, int K, int32_t *idx, void *ws, hipStream_t s) {
+    return select_launch(scores, N, K, idx, ws, OneSeq(), s);
+}
+
+// idx[K]: rows 0 .. first - 1, the K - first - last best of the rows between, rows T - last .. T - 1.
+__global__ __launch_bounds__(kThreads) static void kept_rows_kernel(int32_t *__restrict__ idx, int head, int T, int K) {
+    const int i = blockIdx.x * kThreads + threadIdx.x;
+    if (i < K) idx[i] = i < head ? i : T - K + i;
+}
+int select_kept_launch(const float *scores, int T, int K, int first, int last, int32_t *idx, void *ws, hipStream_t s) {
+    const int pick = K - first - last;
+    if (pick == 0 || K == T) {  // nothing to choose: the rows before `first`, and as many from the end
+        kept_rows_kernel<<<ceil_div(K, kThreads), kThreads, 0, s>>>(idx, K == T ? K : first, T, K);
+        return launch_status();
+    }
+    return select_launch(scores, T - last, pick, idx + first, ws, Kept{first, last}, s);
 }
 
 // ---- the same selection for callers that cannot allocate --------------------------------------

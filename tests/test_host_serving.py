@@ -1,0 +1,196 @@
+"""Refusals of the calls that serve a reduced prefill's rows (packed attention, 4-bit cache, decode steps, eviction): on the
+host, before anything is launched."""
+import ctypes
+
+import pytest
+import torch
+
+import paper_2603_00198_amd as strd
+from paper_2603_00198_amd import binding
+
+P, BIG, F32, BF16 = 0x1000, 1 << 40, 0, 1
+OK, EINVAL, EUNSUPPORTED, EWORKSPACE, EHIP = 0, -1, -2, -3, -4
+
+
+def _seqs(*pairs):
+    return (binding._Seq * max(1, len(pairs)))(*[binding._Seq(n, m, 0) for n, m in pairs])
+
+
+def _cases():
+    nan, inf = float("nan"), float("inf")
+    kv4 = (ctypes.c_void_p * 4)(P, P, P, P)
+    no_v = (ctypes.c_void_p * 4)(P, P, P, None)
+    off = (ctypes.c_void_p * 4)(P, P + 8, P, P)
+    items = (binding._CompactItem * 9)(*[binding._CompactItem(P, P, 64)] * 9)
+    ragged = (binding._CompactItem * 1)(binding._CompactItem(P, P, 6))
+    empty = (binding._CompactItem * 1)(binding._CompactItem(P, None, 64))
+    huge = (binding._CompactItem * 1)(binding._CompactItem(P, P, 1 << 29))
+    two = _seqs((30, 4), (0, 9))
+    a = ctypes.addressof
+    dec = [64, 8, 2, 128, 0.09, 30.0, P, P, P, P, BF16, P, BIG, None]
+    # name -> (consistent arguments, what it returns without a GPU, {position: (value, what the call says to it)})
+    return {
+        "strd_attn_prefill_varlen": (
+            [P, 512, P, 256, P, 256, P, two, 2, 1, 30.0, P, P, 4, 2, 128, 0.09, BF16, None],
+            {0: (None, EINVAL), 1: (511, EINVAL), 2: (None, EINVAL), 3: (255, EINVAL), 4: (None, EINVAL), 5: (-256, EINVAL), 6: (None, EINVAL),
+             7: (None, EINVAL), 8: (0, EINVAL), 10: (-1.0, EINVAL), 13: (3, EINVAL), 14: (0, EINVAL), 15: (0, EINVAL), 16: (0.0, EINVAL), 17: (7, EINVAL)}),
+        "strd_kv4_store": (
+            [P, 256, P, 256, a(kv4), 100, 90, 10, 2, 128, BF16, None],
+            {0: (None, EINVAL), 1: (255, EINVAL), 2: (None, EINVAL), 3: (0, EINVAL), 4: (None, EINVAL), 5: (99, EINVAL), 6: (-1, EINVAL), 7: (11, EINVAL),
+             8: (0, EINVAL), 9: (48, EUNSUPPORTED), 10: (7, EINVAL)}),
+        "strd_kv4_load": (
+            [a(kv4), 100, 90, 10, P, P, 2, 128, F32, None],
+            {0: (None, EINVAL), 1: (99, EINVAL), 2: (-1, EINVAL), 3: (-1, EINVAL), 4: (None, EINVAL), 5: (P + 16, EINVAL), 6: (0, EINVAL),
+             7: (288, EUNSUPPORTED), 8: (2, EINVAL)}),
+        "strd_attn_decode_step_kv4": (
+            [P, a(kv4), P] + dec,
+            {0: (None, EINVAL), 1: (None, EINVAL), 2: (None, EINVAL), 3: (0, EINVAL), 4: (3, EINVAL), 5: (0, EINVAL), 6: (48, EUNSUPPORTED), 7: (0.0, EINVAL),
+             8: (inf, EINVAL), 12: (None, EINVAL), 13: (7, EINVAL), 14: (None, EWORKSPACE), 15: (64, EWORKSPACE)}),
+        "strd_attn_decode_step_weights": (
+            [P, P, P, P] + dec,
+            {0: (None, EINVAL), 1: (None, EINVAL), 2: (None, EINVAL), 3: (None, EINVAL), 4: (0, EINVAL), 5: (3, EINVAL), 6: (0, EINVAL),
+             7: (257, EUNSUPPORTED), 8: (nan, EINVAL), 9: (nan, EINVAL), 13: (None, EINVAL), 14: (-1, EINVAL), 15: (P + 8, EWORKSPACE), 16: (0, EWORKSPACE)}),
+        "strd_cache_evict": (
+            [P, 40000, 900, 4, 100, a(items), 7, None, P, P, P, P, BIG, None],
+            {0: (None, EINVAL), 1: (899, EINVAL), 2: (0, EINVAL), 3: (-1, EINVAL), 4: (897, EINVAL), 5: (a(ragged), EINVAL), 6: (8, EINVAL), 9: (None, EINVAL),
+             11: (None, EWORKSPACE), 12: (1000, EWORKSPACE)}),
+    }, dict(no_v=no_v, off=off, empty=empty, huge=huge, keep=(kv4, items, ragged, two))
+
+
+def _no_gpu():
+    if torch.cuda.is_available():
+        pytest.skip("placeholder pointers: only run without a GPU")
+
+
+def test_inconsistent_arguments_are_refused():
+    _no_gpu()
+    L, (cases, _keep) = binding.lib(), _cases()
+    for name, (good, bad) in cases.items():
+        fn = getattr(L, name)
+        assert len(good) == len(fn.argtypes), name
+        assert fn(*good) == EHIP, name      # past every check; then no GPU, and no fallback
+        for pos, (value, want) in bad.items():
+            args = list(good)
+            args[pos] = value
+            rc = fn(*args)
+            assert rc == want, "%s: argument %d = %r returned %d" % (name, pos, value, rc)
+
+
+def test_descriptors_caches_and_items_are_looked_at():
+    _no_gpu()
+    L, (cases, more) = binding.lib(), _cases()
+    a = ctypes.addressof
+
+    def call(name, **at):
+        args = list(cases[name][0])
+        for k, v in at.items():
+            args[int(k[1:])] = v
+        return getattr(L, name)(*args)
+
+    pf = "strd_attn_prefill_varlen"
+    assert call(pf, _7=_seqs((-1, 4), (3, 3))) == EINVAL
+    assert call(pf, _7=_seqs((1 << 30, 0), (1, 0))) == EINVAL
+    assert call(pf, _7=_seqs((0, 0), (0, 0))) == OK                      # nothing to do
+    assert call(pf, _7=_seqs((0, 0), (0, 0)), _0=None, _6=None) == OK
+    assert call(pf, _8=65, _7=(binding._Seq * 65)(*[binding._Seq(1, 0, 0)] * 65)) == EINVAL
+    assert call(pf, _15=300, _1=4 * 300, _3=600, _5=600) == EUNSUPPORTED
+    assert call(pf, _10=float("inf")) == EINVAL and call(pf, _10=0.0, _11=None, _12=None) == EHIP
+    for name, at in (("strd_kv4_store", "_4"), ("strd_kv4_load", "_0"), ("strd_attn_decode_step_kv4", "_1")):
+        assert call(name, **{at: a(more["no_v"])}) == EINVAL, name
+        assert call(name, **{at: a(more["off"])}) == EINVAL, name
+    assert call("strd_kv4_store", _7=0, _0=None, _2=None) == OK and call("strd_kv4_load", _3=0, _4=None, _5=None) == OK
+    assert call("strd_attn_decode_step_kv4", _11=None, _12=None) == EHIP   # no weights
+    ev = "strd_cache_evict"
+    assert call(ev, _5=a(more["empty"]), _6=1) == EINVAL
+    assert call(ev, _5=a(more["huge"]), _6=1) == EUNSUPPORTED
+    assert call(ev, _5=None, _6=0) == EHIP and call(ev, _5=None, _6=1) == EINVAL
+    assert call(ev, _0=P + 4) == EINVAL
+    assert call(ev, _1=900, _11=None, _12=0) == EHIP                    # up to 32768 rows: no workspace
+
+
+def test_workspaces_follow_the_sizes():
+    L = binding.lib()
+    for name in ("strd_attn_decode_step_kv4_workspace", "strd_attn_decode_step_weights_workspace"):
+        fn = getattr(L, name)
+        assert fn(0, 8, 2, 128, 1, BF16) == 0 and fn(64, 7, 2, 128, 1, BF16) == 0
+        with_w, without = fn(131627, 32, 8, 128, 1, BF16), fn(131627, 32, 8, 128, 0, BF16)
+        assert with_w - without >= 131627 * 32 * 4
+        assert without <= 512 * 32 * 130 * 4 + 256      # splits do not grow with the cache
+    assert L.strd_cache_evict_workspace(30000, 100, 1, 1) == 0
+    assert L.strd_cache_evict_workspace(131627, 100, 1, 1) == L.strd_select_topk_workspace(131626, 98)
+    assert L.strd_cache_evict_workspace(10, 11, 0, 0) == 0
+
+
+def test_kernel_paths():
+    L = binding.lib()
+    path = lambda *a: L.strd_attn_prefill_varlen_kernel_path(*a)
+    assert path(4, 2, 64, F32) == strd.PATH_SIMT and path(4, 2, 96, BF16) == strd.PATH_SIMT
+    assert path(4, 3, 64, BF16) == strd.PATH_NONE and path(4, 2, 300, BF16) == strd.PATH_NONE and path(4, 2, 64, 9) == strd.PATH_NONE
+
+
+def test_binding_refuses_tensors_off_the_gpu_and_other_objects():
+    t3, t2, t1 = torch.zeros(4, 2, 64), torch.zeros(2, 64), torch.zeros(4)
+    with pytest.raises(strd.StrdError):
+        strd.attn_prefill_varlen(t3, t3, t3, [(4, 0, 0)])
+    with pytest.raises(strd.StrdError):
+        strd.attn_decode_step_weights(t2, t3, t3)
+    with pytest.raises(strd.StrdError):
+        strd.cache_evict(t1, 2, 0, 0, [t3])
+    c = strd.Kv4Cache.empty(4, 2, 64, device="cpu")
+    assert c.k_codes.shape == (4, 2, 32) and c.v_meta.shape == (4, 2, 2, 2)
+    for call in (lambda: strd.kv4_store(t3, t3, c, 0), lambda: strd.kv4_load(c, 0, 1), lambda: strd.attn_decode_step_kv4(t2, c, 1),
+                 lambda: strd.kv4_load((1, 2), 0, 1)):
+        with pytest.raises(strd.StrdError):
+            call()
+    with pytest.raises(strd.StrdError):
+        strd.Kv4Cache.empty(4, 2, 48, device="cpu")
+
+
+@pytest.mark.gpu
+def test_binding_refuses_what_does_not_fit_together():
+    d = "cuda"
+    q, k = torch.zeros(10, 4, 64, device=d), torch.zeros(10, 2, 64, device=d)
+    w, c = torch.zeros(10, device=d), strd.Kv4Cache.empty(10, 2, 64)
+    i32 = torch.zeros(10, dtype=torch.int32, device=d)
+    bad = [
+        lambda: strd.attn_prefill_varlen(q, k, k, [(9, 0, 0)]),                       # rows do not add up
+        lambda: strd.attn_prefill_varlen(q, k[:9], k, [(10, 0, 0)]),
+        lambda: strd.attn_prefill_varlen(q, k.bfloat16(), k, [(10, 0, 0)]),
+        lambda: strd.attn_prefill_varlen(q, k.transpose(1, 2), k.transpose(1, 2), [(10, 0, 0)]),
+        lambda: strd.attn_prefill_varlen(q, k.expand(10, 2, 64)[:1].expand(10, 2, 64), k, [(10, 0, 0)]),   # rows on one another
+        lambda: strd.attn_prefill_varlen(q, k, k, [(10, 0, 0)], slopes=torch.zeros(2, device=d)),
+        lambda: strd.attn_prefill_varlen(q, k, k, [(10, 0, 0)], pos=i32[:9]),
+        lambda: strd.attn_prefill_varlen(q, k, k, [(10, 0, 0)], pos=i32.long()),
+        lambda: strd.attn_prefill_varlen(q, k, k, [(10, 0, 0)], cap=-1.0),
+        lambda: strd.attn_prefill_varlen(q, k, k, [(10, 0, 0)], scale=-1.0),
+        lambda: strd.attn_prefill_varlen(q, k, k, [(10, 0, 0)], out=k),
+        lambda: strd.attn_prefill_varlen(q.double(), k.double(), k.double(), [(10, 0, 0)]),
+        lambda: strd.kv4_store(k, k, c, 1),
+        lambda: strd.kv4_store(k, k, c, -1),
+        lambda: strd.kv4_store(q, q, c, 0),
+        lambda: strd.kv4_store(k, k.bfloat16(), c, 0),
+        lambda: strd.kv4_load(c, 5, 6),
+        lambda: strd.kv4_load(c, 0, 1, dtype=torch.float16),
+        lambda: strd.kv4_store(k, k, (c.k_codes, c.k_meta, c.v_codes[:9], c.v_meta), 0),
+        lambda: strd.kv4_store(k, k, (c.k_codes, c.k_codes, c.v_codes, c.v_meta), 0),
+        lambda: strd.attn_decode_step_kv4(q[0], c, 11),
+        lambda: strd.attn_decode_step_kv4(q[0], c, 0),
+        lambda: strd.attn_decode_step_kv4(q[0, :3], c, 4),
+        lambda: strd.attn_decode_step_kv4(q[0], c, 10, weights=w[:9]),
+        lambda: strd.attn_decode_step_kv4(q[0], c, 10, weights=w, want_weights=False),
+        lambda: strd.attn_decode_step_kv4(q[0], c, 10, ws=torch.empty(8, dtype=torch.uint8, device=d)),
+        lambda: strd.attn_decode_step_weights(q[0], k, k, weights_out=i32),
+        lambda: strd.attn_decode_step_weights(q[0], k, k[:9]),
+        lambda: strd.attn_decode_step_weights(q[0], k[:0], k[:0]),
+        lambda: strd.cache_evict(w, 11, 0, 0, [k]),
+        lambda: strd.cache_evict(w, 5, 3, 3, [k]),
+        lambda: strd.cache_evict(w, 5, 0, 0, [k[:9]]),
+        lambda: strd.cache_evict(w, 5, 0, 0, [k] * 8),
+        lambda: strd.cache_evict(w, 5, 0, 0, [k], pos=i32[:9]),
+        lambda: strd.cache_evict(w, 5, 0, 0, [k], outs=[torch.empty(4, 2, 64, device=d)]),
+        lambda: strd.cache_evict(w[1:], 5, 0, 0, []),                                 # not on a 16-byte boundary
+    ]
+    for i, call in enumerate(bad):
+        with pytest.raises(strd.StrdError):
+            call()
+            print("case", i, "was taken")
