@@ -500,37 +500,7 @@ int strd_attn_decode_step(const void *q, const void *k_cache, const void *v_cach
 
 // ------------------------------------------------------------------ packed attention, caches -
 namespace {
-constexpr int kMostRows = 1 << 30;
 inline bool cap_ok(float cap) { return cap >= 0.f && cap < INFINITY; }
-
-// Sequences with rows, longest first, in blocks of `bm` rows; false if the descriptors are inconsistent.
-bool plan_attn(const strd_seq *seqs, int nseq, int bm, AttnTab &t, long long &rows, long long &units) {
-    if (!seqs || nseq < 1 || nseq > STRD_VARLEN_MAX) return false;
-    int order[STRD_VARLEN_MAX], n = 0;
-    long long row0[STRD_VARLEN_MAX];
-    rows = units = 0;
-    for (int b = 0; b < nseq; ++b) {
-        if (seqs[b].N < 0 || seqs[b].M < 0) return false;
-        row0[b] = rows;
-        rows += (long long)seqs[b].N + seqs[b].M;
-        if (rows > kMostRows) return false;
-        if (seqs[b].N + seqs[b].M > 0) order[n++] = b;
-    }
-    std::stable_sort(order, order + n, [&](int a, int b) { return seqs[a].N + seqs[a].M > seqs[b].N + seqs[b].M; });
-    t = AttnTab();
-    t.nseq = n;
-    for (int i = 0; i < n; ++i) {
-        const strd_seq &s = seqs[order[i]];
-        t.row0[i] = (int)row0[order[i]];
-        t.len[i] = s.N + s.M;
-        t.vis[i] = s.N;
-        t.nb[i] = ceil_div(t.len[i], bm);
-        if (i) units += (long long)(t.nb[i - 1] - t.nb[i]) * i;
-        t.base[i] = (int)std::min(units, (long long)kMostRows);
-    }
-    if (n) units += (long long)t.nb[n - 1] * n;
-    return true;
-}
 
 int decode_cache_call(DecCall &a, float scale, float cap, const float *slopes, const int32_t *pos, void *ws, size_t ws_bytes, void *stream) {
     if (a.T < 1 || a.T > kMostRows || a.Hq < 1 || a.Hkv < 1 || a.d < 1 || a.Hq % a.Hkv || !io_ok(a.io) || !(scale > 0.f) || !cap_ok(cap) || !a.q ||
@@ -547,6 +517,7 @@ int decode_cache_call(DecCall &a, float scale, float cap, const float *slopes, c
 
 int strd_attn_prefill_varlen_kernel_path(int Hq, int Hkv, int d, strd_dtype io) {
     if (Hq < 1 || Hkv < 1 || d < 1 || Hq % Hkv || !io_ok(io)) return STRD_PATH_NONE;
+    if (attn_varlen_mfma_supported(Hq, Hkv, d, io)) return STRD_PATH_MFMA;
     return attn_general_supported(d) ? STRD_PATH_SIMT : STRD_PATH_NONE;
 }
 
@@ -563,6 +534,10 @@ int strd_attn_prefill_varlen(const void *q, int64_t ldq, const void *k, int64_t 
     m.scale = scale, m.cap = cap, m.inv_cap = cap > 0.f ? 1.f / cap : 0.f;
     m.slopes = slopes, m.pos = pos, m.prefix = prefix != 0;
     if (!attn_general_supported(d)) return STRD_EUNSUPPORTED;
+    // rows that 16-byte reads do not fit, or a sequence whose keys 32-bit offsets do not reach: the general kernel
+    if (attn_varlen_mfma_supported(Hq, Hkv, d, io) && aligned16(q, k, v, o) && ((ldq | ldk | ldv) & 7) == 0 &&
+        attn_varlen_mfma_reaches(m.tab.len[0], ldk, ldv))
+        return attn_varlen_mfma(q, k, v, o, Hq, Hkv, d, m, seqs, nseq, as_stream(stream));
     return attn_varlen_general(q, k, v, o, Hq, Hkv, d, m, units, io, as_stream(stream));
 }
 

@@ -1,5 +1,7 @@
 // Packed batches of sequences for attention: which rows a workgroup takes, and how scores are changed.
 #pragma once
+#include <algorithm>
+
 #include "common.h"
 
 namespace strd {
@@ -19,6 +21,37 @@ struct AttnTab {
         s = rem - row * (top + 1);
     }
 };
+
+constexpr int kMostRows = 1 << 30;
+
+// Sequences with rows, longest first, in blocks of `bm` rows; false if the descriptors are inconsistent.
+inline bool plan_attn(const strd_seq *seqs, int nseq, int bm, AttnTab &t, long long &rows, long long &units) {
+    if (!seqs || nseq < 1 || nseq > STRD_VARLEN_MAX) return false;
+    int order[STRD_VARLEN_MAX], n = 0;
+    long long row0[STRD_VARLEN_MAX];
+    rows = units = 0;
+    for (int b = 0; b < nseq; ++b) {
+        if (seqs[b].N < 0 || seqs[b].M < 0) return false;
+        row0[b] = rows;
+        rows += (long long)seqs[b].N + seqs[b].M;
+        if (rows > kMostRows) return false;
+        if (seqs[b].N + seqs[b].M > 0) order[n++] = b;
+    }
+    std::stable_sort(order, order + n, [&](int a, int b) { return seqs[a].N + seqs[a].M > seqs[b].N + seqs[b].M; });
+    t = AttnTab();
+    t.nseq = n;
+    for (int i = 0; i < n; ++i) {
+        const strd_seq &s = seqs[order[i]];
+        t.row0[i] = (int)row0[order[i]];
+        t.len[i] = s.N + s.M;
+        t.vis[i] = s.N;
+        t.nb[i] = ceil_div(t.len[i], bm);
+        if (i) units += (long long)(t.nb[i - 1] - t.nb[i]) * i;
+        t.base[i] = (int)std::min(units, (long long)kMostRows);
+    }
+    if (n) units += (long long)t.nb[n - 1] * n;
+    return true;
+}
 
 struct AttnMod {
     AttnTab tab;

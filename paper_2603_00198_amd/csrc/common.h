@@ -329,6 +329,9 @@ int ssd_mfma(const void *x, const float *dt, const float *A, const void *B, cons
 
 struct AttnMod;  // attn_varlen.h
 bool attn_varlen_mfma_supported(int Hq, int Hkv, int d, strd_dtype io);
+bool attn_varlen_mfma_reaches(int longest, long long ldk, long long ldv);
+int attn_varlen_mfma(const void *q, const void *k, const void *v, void *o, int Hq, int Hkv, int d, const AttnMod &mod, const strd_seq *seqs,
+                     int nseq, hipStream_t st);
 int attn_varlen_general(const void *q, const void *k, const void *v, void *o, int Hq, int Hkv, int d, const AttnMod &mod, long long units,
                         strd_dtype io, hipStream_t st);
 int kv4_store_launch(const void *k, long long ldk, const void *v, long long ldv, const strd_kv4 &c, int row0, int R, int Hkv, int d,

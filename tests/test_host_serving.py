@@ -128,6 +128,23 @@ def test_kernel_paths():
     assert path(4, 3, 64, BF16) == strd.PATH_NONE and path(4, 2, 300, BF16) == strd.PATH_NONE and path(4, 2, 64, 9) == strd.PATH_NONE
 
 
+def test_kernels_with_split_lds_reads_do_not_spill():
+    """attn_varlen_mfma.hip waits for transposing LDS reads later than it issues them: a spill between the two would save what is
+    not there yet (the compiler's own resource report)."""
+    import os
+    import re
+    import subprocess
+
+    from paper_2603_00198_amd import build as strd_build
+    src = os.path.join(strd_build.CSRC, "attn_varlen_mfma.hip")
+    r = subprocess.run([strd_build.HIPCC] + strd_build.FLAGS + ["--cuda-device-only", "-c", src, "-o", os.devnull,
+                                                                "-Rpass-analysis=kernel-resource-usage"], capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr[-2000:]
+    for what in (r"ScratchSize \[bytes/lane\]", "VGPRs Spill", "SGPRs Spill", "AGPRs"):
+        vals = [int(v) for v in re.findall(what + r": (\d+)", r.stderr)]
+        assert vals and not any(vals), (what, vals)
+
+
 def test_binding_refuses_tensors_off_the_gpu_and_other_objects():
     t3, t2, t1 = torch.zeros(4, 2, 64), torch.zeros(2, 64), torch.zeros(4)
     with pytest.raises(strd.StrdError):
