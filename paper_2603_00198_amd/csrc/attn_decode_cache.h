@@ -46,6 +46,9 @@ struct DecCall {
     bool kv4;
 };
 
+bool dec_mfma_supported(int Hq, int Hkv, int d, bool kv4, strd_dtype io);
+int dec_mfma_splits(int T, int Hkv, int &tps);
+void dec_mfma(const DecCall &a, const DecWs &ws, int nsplit, int tps, hipStream_t st);
 int dec_splits_general(int T, int Hq, int Hkv, int &tps);
 int dec_combine(const DecCall &a, const DecWs &ws, int nsplit, hipStream_t st);
 

@@ -293,21 +293,23 @@ int dec_combine(const DecCall &a, const DecWs &ws, int nsplit, hipStream_t st) {
 }
 
 size_t attn_decode_cache_ws(int T, int Hq, int Hkv, int d, bool kv4, bool weights, strd_dtype io) {
-    (void)kv4;
-    (void)io;
-    int tps;
-    return dec_ws_bytes(dec_splits_general(T, Hq, Hkv, tps), Hq, d, dec_ldt(T), weights);
+    // (a plain cache that 16-byte reads do not fit takes the general kernel whatever its shape: room for either's splits)
+    int tps, n = dec_splits_general(T, Hq, Hkv, tps);
+    if (dec_mfma_supported(Hq, Hkv, d, kv4, io)) n = kv4 ? dec_mfma_splits(T, Hkv, tps) : max(n, dec_mfma_splits(T, Hkv, tps));
+    return dec_ws_bytes(n, Hq, d, dec_ldt(T), weights);
 }
 
 int attn_decode_cache(const DecCall &a, void *wsp, hipStream_t st) {
+    const bool mfma = dec_mfma_supported(a.Hq, a.Hkv, a.d, a.kv4, a.io) && (((uintptr_t)a.q | (uintptr_t)a.c.k | (uintptr_t)a.c.v) & 15) == 0;
     DecWs ws;
     int tps;
-    const int nsplit = dec_splits_general(a.T, a.Hq, a.Hkv, tps);
+    const int nsplit = mfma ? dec_mfma_splits(a.T, a.Hkv, tps) : dec_splits_general(a.T, a.Hq, a.Hkv, tps);
     ws.ml = (float *)wsp;  // (pairs: they come first)
     ws.part = ws.ml + (size_t)nsplit * a.Hq * 2;
     ws.ldt = dec_ldt(a.T);
     ws.scores = a.w_out ? (float *)((char *)wsp + align_up((size_t)nsplit * a.Hq * (a.d + 2) * sizeof(float), 256)) : nullptr;
-    if (a.io == STRD_BF16) launch_typed<bf16_t>(a, ws, nsplit, tps, st);
+    if (mfma) dec_mfma(a, ws, nsplit, tps, st);
+    else if (a.io == STRD_BF16) launch_typed<bf16_t>(a, ws, nsplit, tps, st);
     else launch_typed<float>(a, ws, nsplit, tps, st);
     if (hipGetLastError() != hipSuccess) return STRD_EHIP;
     return dec_combine(a, ws, nsplit, st);
