@@ -46,6 +46,15 @@ struct DecCall {
     bool kv4;
 };
 
+// Workgroup b runs on XCD b % 8, each with an L2 of its own: the kv heads of one split, which share lines of the cache -- a row's
+// (s, z) pairs of 8 heads of 128 channels are one line -- go to one XCD, one after the other.
+__device__ __forceinline__ void dec_place(int b, int Hkv, int &hk, int &split) {
+    const int u = b / kXcd;
+    hk = u % Hkv;
+    split = b % kXcd + kXcd * (u / Hkv);
+}
+inline int dec_grid(int Hkv, int nsplit) { return Hkv * ((nsplit + kXcd - 1) / kXcd * kXcd); }
+
 bool dec_mfma_supported(int Hq, int Hkv, int d, bool kv4, strd_dtype io);
 int dec_mfma_splits(int T, int Hkv, int &tps);
 void dec_mfma(const DecCall &a, const DecWs &ws, int nsplit, int tps, hipStream_t st);

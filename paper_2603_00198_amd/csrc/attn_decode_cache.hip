@@ -52,10 +52,13 @@ __device__ __forceinline__ void load8(const void *rows, const void *meta, size_t
 
 template <typename T, bool KV4, bool VEC, int RP, int NC>
 __global__ __launch_bounds__(kThreads) void decode_cache_kernel(const T *__restrict__ q, CacheView c, DecWs ws, int Tn, int Hq, int Hkv,
-                                                                int d, int tps, ScoreMod mod) {
+                                                                int d, int tps, int nsplit, ScoreMod mod) {
     extern __shared__ float sm_acc[];  // [kGroups][d]
     __shared__ float sm_m[kGroups][RP], sm_l[kGroups][RP];
-    const int hk = blockIdx.x, split = blockIdx.y, rep = Hq / Hkv, r0 = blockIdx.z * RP;
+    int hk, split;
+    dec_place(blockIdx.x, Hkv, hk, split);
+    if (split >= nsplit) return;  // uniform
+    const int rep = Hq / Hkv, r0 = blockIdx.y * RP;
     const int grp = threadIdx.x / kLanes, sub = threadIdx.x % kLanes;
     const int nh = min(RP, rep - r0), h0 = hk * rep + r0;
     float qv[RP][NC][8], acc[RP][NC][8], m[RP], l[RP], slope[RP];
@@ -167,94 +170,129 @@ __global__ __launch_bounds__(kThreads) void decode_cache_kernel(const T *__restr
     }
 }
 
-// Reference and reciprocal sum of one head over all splits, by the 64 lanes of a wave.
-__device__ __forceinline__ void head_total(const float *__restrict__ ml, int nsplit, int Hq, int h, float &mx, float &den) {
-    const int lane = threadIdx.x % kWave;
-    float2 pr[kDecMaxSplits / kWave];
-    mx = kDecNegBig;
+// References and reciprocal sums of 32 heads from h0 on over all splits, 8 lanes a head, by a workgroup: everything is asked
+// for before the first maximum.  hm, hl hold them behind the barrier at the end.
+constexpr int kHeadsAtOnce = kThreads / 8, kSplitLoads = 16;
+__device__ __forceinline__ void head_totals(const float *__restrict__ ml, int nsplit, int Hq, int h0, float *hm, float *hl) {
+    const int h = min(h0 + (int)threadIdx.x / 8, Hq - 1), sub = threadIdx.x % 8;
+    const float2 *pairs = reinterpret_cast<const float2 *>(ml) + h;
+    float mx = kDecNegBig, den = 0.f;
+    for (int s0 = 0; s0 < nsplit; s0 += 8 * kSplitLoads) {  // (one round up to 128 splits)
+        float2 pr[kSplitLoads];
 #pragma unroll
-    for (int i = 0; i < kDecMaxSplits / kWave; ++i) {
-        if (i * kWave >= nsplit) break;  // uniform
-        pr[i] = *reinterpret_cast<const float2 *>(ml + ((size_t)min(lane + kWave * i, nsplit - 1) * Hq + h) * 2);
-        mx = fmaxf(mx, pr[i].x);
+        for (int i = 0; i < kSplitLoads; ++i) pr[i] = pairs[(size_t)min(s0 + sub + 8 * i, nsplit - 1) * Hq];
+        float nm = mx;
+#pragma unroll
+        for (int i = 0; i < kSplitLoads; ++i) nm = fmaxf(nm, pr[i].x);
+        den *= ex2(mx - nm);
+#pragma unroll
+        for (int i = 0; i < kSplitLoads; ++i)
+            if (s0 + sub + 8 * i < nsplit) den = fmaf(ex2(pr[i].x - nm), pr[i].y, den);
+        mx = nm;
     }
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o, kWave));
-    den = 0.f;
-#pragma unroll
-    for (int i = 0; i < kDecMaxSplits / kWave; ++i) {
-        if (i * kWave >= nsplit) break;
-        if (lane + kWave * i < nsplit) den = fmaf(ex2(pr[i].x - mx), pr[i].y, den);
+    for (int o = 4; o > 0; o >>= 1) {
+        const float om = __shfl_xor(mx, o, kWave), od = __shfl_xor(den, o, kWave), nm = fmaxf(mx, om);
+        den = den * ex2(mx - nm) + od * ex2(om - nm);
+        mx = nm;
     }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) den += __shfl_xor(den, o, kWave);
+    if (sub == 0) {
+        hm[threadIdx.x / 8] = mx;
+        hl[threadIdx.x / 8] = 1.f / den;
+    }
+    __syncthreads();
 }
 
-constexpr int kHeadsAtOnce = 64, kTokPerBlock = 4 * kThreads;
+// One workgroup per 32 channels of a head (8 lane groups share the splits), then one per 1024 tokens' weights.
+constexpr int kTokPerBlock = 4 * kThreads, kPartLoads = 16;
 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void decode_combine_kernel(DecWs ws, T *__restrict__ o, const float *__restrict__ w_in,
                                                                   float *__restrict__ w_out, int nsplit, int Tn, int Hq, int d,
                                                                   int o_blocks) {
-    __shared__ float wts[kDecMaxSplits], tot[2], sums[8][33], hm[kHeadsAtOnce], hl[kHeadsAtOnce];
-    const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+    __shared__ float sums[8][33], dens[8], maxs[8], hm[kHeadsAtOnce], hl[kHeadsAtOnce];
+    const int tid = threadIdx.x;
     if ((int)blockIdx.x < o_blocks) {
         const int per = (d + 31) / 32, h = blockIdx.x / per, c = (blockIdx.x % per) * 32 + tid % 32, sg = tid / 32;
-        if (wave == 0) {
-            float mx, den;
-            head_total(ws.ml, nsplit, Hq, h, mx, den);
-            for (int s = lane; s < nsplit; s += kWave) wts[s] = ex2(ws.ml[((size_t)s * Hq + h) * 2] - mx);
-            if (lane == 0) tot[0] = den;
+        const float2 *pairs = reinterpret_cast<const float2 *>(ws.ml) + h;
+        const float *part = ws.part + (size_t)h * d + min(c, d - 1);
+        float mx = kDecNegBig, den = 0.f, acc = 0.f;  // of this lane group's splits; everything is asked for before the first sum
+        for (int s0 = sg; s0 < nsplit; s0 += 8 * kPartLoads) {
+            float2 pr[kPartLoads];
+            float v[kPartLoads];
+#pragma unroll
+            for (int i = 0; i < kPartLoads; ++i) {
+                const size_t at = (size_t)min(s0 + 8 * i, nsplit - 1) * Hq;
+                pr[i] = pairs[at];
+                v[i] = part[at * d];
+            }
+            float nm = mx;
+#pragma unroll
+            for (int i = 0; i < kPartLoads; ++i) nm = fmaxf(nm, pr[i].x);
+            const float corr = ex2(mx - nm);
+            den *= corr;
+            acc *= corr;
+#pragma unroll
+            for (int i = 0; i < kPartLoads; ++i) {
+                const float f = s0 + 8 * i < nsplit ? ex2(pr[i].x - nm) : 0.f;
+                den = fmaf(f, pr[i].y, den);
+                acc = fmaf(f, s0 + 8 * i < nsplit ? v[i] : 0.f, acc);
+            }
+            mx = nm;
+        }
+        sums[sg][tid % 32] = acc;
+        if (tid % 32 == 0) {
+            dens[sg] = den;
+            maxs[sg] = mx;
         }
         __syncthreads();
-        float acc = 0.f;
-        if (c < d)
-            for (int s = sg; s < nsplit; s += 8) acc = fmaf(wts[s], ws.part[((size_t)s * Hq + h) * d + c], acc);
-        sums[sg][tid % 32] = acc;
-        __syncthreads();
         if (tid < 32 && c < d) {
-            float num = 0.f;
+            float top = maxs[0], num = 0.f, all = 0.f;
 #pragma unroll
-            for (int g = 0; g < 8; ++g) num += sums[g][tid];  // fixed order
-            o[(size_t)h * d + c] = from_f32<T>(num / tot[0]);
+            for (int g = 1; g < 8; ++g) top = fmaxf(top, maxs[g]);
+#pragma unroll
+            for (int g = 0; g < 8; ++g) {  // fixed order
+                const float f = ex2(maxs[g] - top);
+                num = fmaf(f, sums[g][tid], num);
+                all = fmaf(f, dens[g], all);
+            }
+            o[(size_t)h * d + c] = from_f32<T>(num / all);
         }
         return;
     }
-    const long long t0 = (long long)(blockIdx.x - o_blocks) * kTokPerBlock + tid;
-    float acc[4] = {0.f, 0.f, 0.f, 0.f};
+    const long long t0 = (long long)(blockIdx.x - o_blocks) * kTokPerBlock + 4 * tid;  // (rows of scores are padded to 64)
+    const bool live = t0 < Tn;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int h0 = 0; h0 < Hq; h0 += kHeadsAtOnce) {
         const int nh = min(kHeadsAtOnce, Hq - h0);
-        __syncthreads();
-        for (int h = wave; h < nh; h += kThreads / kWave) {
-            float mx, den;
-            head_total(ws.ml, nsplit, Hq, h0 + h, mx, den);
-            if (lane == 0) {
-                hm[h] = mx;
-                hl[h] = 1.f / den;
-            }
-        }
-        __syncthreads();
+        if (h0) __syncthreads();
+        head_totals(ws.ml, nsplit, Hq, h0, hm, hl);
+        if (!live) continue;
+        const float *s = ws.scores + (size_t)h0 * ws.ldt + t0;
+#pragma unroll 8
         for (int h = 0; h < nh; ++h) {
-            const float *s = ws.scores + (size_t)(h0 + h) * ws.ldt;
-#pragma unroll
-            for (int u = 0; u < 4; ++u) acc[u] = fmaf(ex2(s[min(t0 + kThreads * u, (long long)Tn - 1)] - hm[h]), hl[h], acc[u]);
+            const float4 x = *reinterpret_cast<const float4 *>(s + (size_t)h * ws.ldt);
+            const float m = hm[h], l = hl[h];
+            acc.x = fmaf(ex2(x.x - m), l, acc.x);
+            acc.y = fmaf(ex2(x.y - m), l, acc.y);
+            acc.z = fmaf(ex2(x.z - m), l, acc.z);
+            acc.w = fmaf(ex2(x.w - m), l, acc.w);
         }
     }
+    const float a[4] = {acc.x, acc.y, acc.z, acc.w};
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-        const long long t = t0 + kThreads * u;
-        if (t < Tn) w_out[t] = (w_in ? w_in[t] : 0.f) + acc[u] / (float)Hq;
-    }
+    for (int u = 0; u < 4; ++u)
+        if (t0 + u < Tn) w_out[t0 + u] = (w_in ? w_in[t0 + u] : 0.f) + a[u] / (float)Hq;
 }
 
 template <typename T, bool KV4, bool VEC, int RP>
 void launch_rp(const DecCall &a, const DecWs &ws, int nsplit, int tps, hipStream_t st) {
-    const dim3 grid(a.Hkv, nsplit, ceil_div(a.Hq / a.Hkv, RP));
+    const dim3 grid(dec_grid(a.Hkv, nsplit), ceil_div(a.Hq / a.Hkv, RP));
     const size_t smem = (size_t)kGroups * a.d * sizeof(float);
     if (a.d <= 128)
-        decode_cache_kernel<T, KV4, VEC, RP, 1><<<grid, kThreads, smem, st>>>((const T *)a.q, a.c, ws, a.T, a.Hq, a.Hkv, a.d, tps, a.mod);
+        decode_cache_kernel<T, KV4, VEC, RP, 1><<<grid, kThreads, smem, st>>>((const T *)a.q, a.c, ws, a.T, a.Hq, a.Hkv, a.d, tps, nsplit, a.mod);
     else
-        decode_cache_kernel<T, KV4, VEC, RP, 2><<<grid, kThreads, smem, st>>>((const T *)a.q, a.c, ws, a.T, a.Hq, a.Hkv, a.d, tps, a.mod);
+        decode_cache_kernel<T, KV4, VEC, RP, 2><<<grid, kThreads, smem, st>>>((const T *)a.q, a.c, ws, a.T, a.Hq, a.Hkv, a.d, tps, nsplit, a.mod);
 }
 
 template <typename T, bool KV4, bool VEC>

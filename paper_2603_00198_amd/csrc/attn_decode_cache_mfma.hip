@@ -66,12 +66,15 @@ struct Shape {
 
 template <int D, bool KV4, int NP, bool BIAS>
 __global__ __launch_bounds__(kWaves *kWave) __attribute__((amdgpu_waves_per_eu(NP == 1 && !BIAS && (KV4 || D == 64) ? 3 : 2))) void decode_cache_mfma_kernel(
-    const bf16_t *__restrict__ q, CacheView cv, DecWs ws, int Tn, int Hq, int Hkv, int tps, ScoreMod mod) {
+    const bf16_t *__restrict__ q, CacheView cv, DecWs ws, int Tn, int Hq, int Hkv, int tps, int nsplit, ScoreMod mod) {
     using S = Shape<D, KV4>;
     constexpr int NG = S::kGroupsOfD, HP = S::kHeads, KS = S::kKSteps, VT = S::kVTiles, KD = S::kKDwords, VD = S::kVDwords;
     __shared__ __attribute__((aligned(16))) float sm_o[kWaves][HP][D];
     __shared__ float sm_m[kWaves][HP], sm_l[kWaves][HP];
-    const int hk = blockIdx.x, split = blockIdx.y, rep = Hq / Hkv;
+    int hk, split;
+    dec_place(blockIdx.x, Hkv, hk, split);
+    if (split >= nsplit) return;  // uniform
+    const int rep = Hq / Hkv;
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int lr = lane & 15, c = lane >> 4;
     const int grp = lr / HP, hcol = lr % HP;               // this lane's column: group of channels, head
@@ -410,11 +413,11 @@ __global__ __launch_bounds__(kWaves *kWave) __attribute__((amdgpu_waves_per_eu(N
 
 template <int D, bool KV4, int NP>
 void launch_bias(const DecCall &a, const DecWs &ws, int nsplit, int tps, hipStream_t st) {
-    const dim3 grid(a.Hkv, nsplit);
+    const int grid = dec_grid(a.Hkv, nsplit);
     if (a.mod.slopes)
-        decode_cache_mfma_kernel<D, KV4, NP, true><<<grid, kWaves * kWave, 0, st>>>((const bf16_t *)a.q, a.c, ws, a.T, a.Hq, a.Hkv, tps, a.mod);
+        decode_cache_mfma_kernel<D, KV4, NP, true><<<grid, kWaves * kWave, 0, st>>>((const bf16_t *)a.q, a.c, ws, a.T, a.Hq, a.Hkv, tps, nsplit, a.mod);
     else
-        decode_cache_mfma_kernel<D, KV4, NP, false><<<grid, kWaves * kWave, 0, st>>>((const bf16_t *)a.q, a.c, ws, a.T, a.Hq, a.Hkv, tps, a.mod);
+        decode_cache_mfma_kernel<D, KV4, NP, false><<<grid, kWaves * kWave, 0, st>>>((const bf16_t *)a.q, a.c, ws, a.T, a.Hq, a.Hkv, tps, nsplit, a.mod);
 }
 
 }  // namespace

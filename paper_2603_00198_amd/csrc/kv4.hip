@@ -33,57 +33,79 @@ struct Side {
     long long ld;        // elements between rows
 };
 
-// VEC: 8 elements of a row can be read as one vector.
-template <typename T, bool VEC>
-__global__ __launch_bounds__(kThreads) void kv4_store_kernel(Side k, Side v, long long units, int upr) {
-    typedef typename Vec8<T>::type V;
-    const Side &sd = blockIdx.y ? v : k;
-    const long long u = (long long)blockIdx.x * kThreads + threadIdx.x;  // 8 channels; 4 lanes a group, never half of one
-    if (u >= units) return;
-    const long long row = u / upr;
-    const int c = (int)(u - row * upr);
-    const T *src = (const T *)sd.rows + row * sd.ld + 8 * c;
-    float x[8];
-    if constexpr (VEC) {
-        const V t = *reinterpret_cast<const V *>(src);
+constexpr int kUnits = 2;  // pieces of 8 channels a lane has on their way
+
+// The dword of codes of this lane's 8 values; (s, z) of its group, which it shares with the other lanes of its quad.
+__device__ __forceinline__ uint32_t quantize(const float (&x)[8], uint32_t &meta) {
+    // (minimum and maximum that keep a NaN: two values an instruction, and no look at single values)
+    float lo = x[0], hi = x[0];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = to_f32((T)t[e]);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = to_f32(src[e]);
+    for (int e = 1; e < 8; ++e) {
+        lo = __builtin_elementwise_minimum(lo, x[e]);
+        hi = __builtin_elementwise_maximum(hi, x[e]);
     }
-    float lo = x[0], hi = x[0], odd = 0.f;  // odd: NaN if a value is not finite
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        lo = fminf(lo, x[e]);
-        hi = fmaxf(hi, x[e]);
-        odd = fmaf(x[e], 0.f, odd);
-    }
-    lo = fminf(lo, quad<kSwap1>(lo));
-    hi = fmaxf(hi, quad<kSwap1>(hi));
-    odd += quad<kSwap1>(odd);
-    lo = fminf(lo, quad<kSwap2>(lo));
-    hi = fmaxf(hi, quad<kSwap2>(hi));
-    odd += quad<kSwap2>(odd);
+    lo = __builtin_elementwise_minimum(lo, quad<kSwap1>(lo));
+    hi = __builtin_elementwise_maximum(hi, quad<kSwap1>(hi));
+    lo = __builtin_elementwise_minimum(lo, quad<kSwap2>(lo));
+    hi = __builtin_elementwise_maximum(hi, quad<kSwap2>(hi));
     float s = bf16_round((hi - lo) / 15.f);
-    const bool off = !(odd == 0.f) || !(s < INFINITY);
+    const bool off = !(s < INFINITY);  // infinities and NaN are in the difference
     s = s < kKv4Tiny ? 0.f : s;
     const float z = bf16_round(lo + 8.f * s);
     const bool bad = off || !(fabsf(z) < INFINITY);  // (bf16 ends below fp32's largest numbers)
     // (x - z) / s, correctly rounded: s has 8 bits and is no denormal, r is its correctly rounded reciprocal, and one residual
-    // of the first quotient gives the second (Markstein), which is what a division would return
+    // of the first quotient gives the second (Markstein), which is what a division would return.  Clamped to -8 .. 7 it is
+    // rounded to a whole number, ties to even, by adding 1.5 * 2^23; that and 8 leaves the code in the sum's low bits, and the eight
+    // sums, shifted to their places, add up to the dword and a constant.
     const float r = s > 0.f ? 1.f / s : 0.f;
-    uint32_t codes = 0;
+    constexpr float kRound = 12582912.f + 8.f;
+    uint32_t codes = 0u - 0x4B400000u * 0x11111111u;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         const float d = x[e] - z, q0 = d * r, q = fmaf(fmaf(-q0, s, d), r, q0);
-        const float n = fminf(fmaxf(rintf(q) + 8.f, 0.f), 15.f);  // (NaN becomes 0)
-        codes |= (uint32_t)n << (4 * e);
+        codes += __builtin_bit_cast(uint32_t, __builtin_amdgcn_fmed3f(q, -8.f, 7.f) + kRound) << (4 * e);
     }
-    reinterpret_cast<uint32_t *>(sd.codes)[u] = codes;
-    if ((c & 3) == 0)
-        reinterpret_cast<uint32_t *>(sd.meta)[u / 4] = bad ? 0x7FC07FC0u : bf16_bits(s) | bf16_bits(z) << 16;
+    meta = bad ? 0x7FC07FC0u : bf16_bits(s) | bf16_bits(z) << 16;
+    return codes;
 }
+
+// VEC: 8 elements of a row can be read as one vector.  DENSE: rows lie one behind the other, and a lane's pieces need no division.
+template <typename T, bool VEC, bool DENSE>
+__global__ __launch_bounds__(kThreads) void kv4_store_kernel(Side k, Side v, long long units, int upr) {
+    typedef typename Vec8<T>::type V;
+    const Side &sd = blockIdx.y ? v : k;
+    const long long u0 = (long long)blockIdx.x * (kThreads * kUnits) + threadIdx.x;  // 8 channels; 4 lanes a group, never half of one
+    V t[kUnits];
+    float x[kUnits][8];
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+        const long long u = min(u0 + kThreads * i, units - 1);
+        const T *src = (const T *)sd.rows + 8 * u;
+        if constexpr (!DENSE) {
+            const long long row = u / upr;
+            src = (const T *)sd.rows + row * sd.ld + 8 * (u - row * upr);
+        }
+        if constexpr (VEC) {
+            t[i] = *reinterpret_cast<const V *>(src);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[i][e] = to_f32(src[e]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+        const long long u = u0 + kThreads * i;
+        if constexpr (VEC)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[i][e] = to_f32((T)t[i][e]);
+        uint32_t meta;
+        const uint32_t codes = quantize(x[i], meta);
+        if (u >= units) continue;  // (the four lanes of a group are on one side of the end)
+        reinterpret_cast<uint32_t *>(sd.codes)[u] = codes;
+        if ((u & 3) == 0) reinterpret_cast<uint32_t *>(sd.meta)[u / 4] = meta;
+    }
+}
+
 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void kv4_load_kernel(const uint32_t *__restrict__ kc, const uint32_t *__restrict__ km,
@@ -106,18 +128,20 @@ int kv4_store_launch(const void *k, long long ldk, const void *v, long long ldv,
                      strd_dtype io, hipStream_t st) {
     const int upr = Hkv * (d / 8);
     const long long units = (long long)R * upr, first = (long long)row0 * upr;
-    const dim3 grid((unsigned)((units + kThreads - 1) / kThreads), 2);
+    const dim3 grid((unsigned)((units + kThreads * kUnits - 1) / (kThreads * kUnits)), 2);
     const Side sk = {k, (uint32_t *)c.k_codes + first, (uint32_t *)c.k_meta + first / 4, ldk};
     const Side sv = {v, (uint32_t *)c.v_codes + first, (uint32_t *)c.v_meta + first / 4, ldv};
     const size_t al = 8 * (io == STRD_BF16 ? 2 : 4);
-    const bool vec = !((uintptr_t)k % al) && !((uintptr_t)v % al) && ldk % 8 == 0 && ldv % 8 == 0;
-    if (io == STRD_BF16) {
-        if (vec) kv4_store_kernel<bf16_t, true><<<grid, kThreads, 0, st>>>(sk, sv, units, upr);
-        else kv4_store_kernel<bf16_t, false><<<grid, kThreads, 0, st>>>(sk, sv, units, upr);
-    } else {
-        if (vec) kv4_store_kernel<float, true><<<grid, kThreads, 0, st>>>(sk, sv, units, upr);
-        else kv4_store_kernel<float, false><<<grid, kThreads, 0, st>>>(sk, sv, units, upr);
-    }
+    const bool dense = (ldk == (long long)Hkv * d && ldv == ldk) || R == 1;
+    const bool vec = !((uintptr_t)k % al) && !((uintptr_t)v % al) && (dense || (ldk % 8 == 0 && ldv % 8 == 0));
+    auto launch = [&](auto *tag) {
+        using T = std::remove_pointer_t<decltype(tag)>;
+        if (vec && dense) kv4_store_kernel<T, true, true><<<grid, kThreads, 0, st>>>(sk, sv, units, upr);
+        else if (vec) kv4_store_kernel<T, true, false><<<grid, kThreads, 0, st>>>(sk, sv, units, upr);
+        else kv4_store_kernel<T, false, false><<<grid, kThreads, 0, st>>>(sk, sv, units, upr);
+    };
+    if (io == STRD_BF16) launch((bf16_t *)nullptr);
+    else launch((float *)nullptr);
     return launch_status();
 }
 
