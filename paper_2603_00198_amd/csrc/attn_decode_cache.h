@@ -55,7 +55,7 @@ __device__ __forceinline__ void dec_place(int b, int Hkv, int &hk, int &split) {
 }
 inline int dec_grid(int Hkv, int nsplit) { return Hkv * ((nsplit + kXcd - 1) / kXcd * kXcd); }
 
-bool dec_mfma_supported(int Hq, int Hkv, int d, bool kv4, strd_dtype io);
+bool dec_mfma_supported(int T, int Hq, int Hkv, int d, bool kv4, strd_dtype io);
 int dec_mfma_splits(int T, int Hkv, int &tps);
 void dec_mfma(const DecCall &a, const DecWs &ws, int nsplit, int tps, hipStream_t st);
 int dec_splits_general(int T, int Hq, int Hkv, int &tps);

@@ -333,12 +333,12 @@ int dec_combine(const DecCall &a, const DecWs &ws, int nsplit, hipStream_t st) {
 size_t attn_decode_cache_ws(int T, int Hq, int Hkv, int d, bool kv4, bool weights, strd_dtype io) {
     // (a plain cache that 16-byte reads do not fit takes the general kernel whatever its shape: room for either's splits)
     int tps, n = dec_splits_general(T, Hq, Hkv, tps);
-    if (dec_mfma_supported(Hq, Hkv, d, kv4, io)) n = kv4 ? dec_mfma_splits(T, Hkv, tps) : max(n, dec_mfma_splits(T, Hkv, tps));
+    if (dec_mfma_supported(T, Hq, Hkv, d, kv4, io)) n = kv4 ? dec_mfma_splits(T, Hkv, tps) : max(n, dec_mfma_splits(T, Hkv, tps));
     return dec_ws_bytes(n, Hq, d, dec_ldt(T), weights);
 }
 
 int attn_decode_cache(const DecCall &a, void *wsp, hipStream_t st) {
-    const bool mfma = dec_mfma_supported(a.Hq, a.Hkv, a.d, a.kv4, a.io) && (((uintptr_t)a.q | (uintptr_t)a.c.k | (uintptr_t)a.c.v) & 15) == 0;
+    const bool mfma = dec_mfma_supported(a.T, a.Hq, a.Hkv, a.d, a.kv4, a.io) && (((uintptr_t)a.q | (uintptr_t)a.c.k | (uintptr_t)a.c.v) & 15) == 0;
     DecWs ws;
     int tps;
     const int nsplit = mfma ? dec_mfma_splits(a.T, a.Hkv, tps) : dec_splits_general(a.T, a.Hq, a.Hkv, tps);

@@ -5,17 +5,19 @@
 // turning codes into numbers and multiplying them into up to 8 heads one by one takes six.  So both products are matrix products,
 // on codes as they are:
 //  * A code n becomes the bf16 number 16 + n by a shift and one instruction (its bits are the upper mantissa bits; exact).
-//  * Scores: A = the codes of 16 rows, B = the query heads, a column for every (group of channels, head) with zeros outside the group.
-//    The product leaves every group's sum of q (16 + n) apart; with the group's s and z it becomes s * sum + (z - 24 s) * sum q,
-//    and the groups of a head, columns 4 (8) lanes apart, are added by two rotations of the 16 lanes.  An accumulator's rows are
-//    rows of the cache, four to a lane: the next product's operand as it stands.
-//  * Values: A = the codes of V with the cache's rows as the contraction index, B = p * s, rounded to bf16 -- the one rounding of
-//    the path beside the output's -- for every (group, head).  A lane collects 8 rows' codes and
-//    regroups their halves.  What the 24 too many and z add does not depend on the channel: each lane sums p z - 24 (the rounded
-//    p s) in fp32.  Rows (channels) of the product and columns of another group belong to nobody.
+//  * Scores: A = the codes of 16 rows, B = the query heads, a column for every (head, group of channels) with zeros outside the
+//    group, and -24 sum q to start from.  The product leaves every group's sum of q (n - 8) apart; with the group's s and z it becomes
+//    s * sum + z * sum q.  An accumulator's rows are rows of the cache, four to a lane, and the groups of a head are neighbouring
+//    lanes: they exchange their parts so that each ends up with the whole score of one row of the four (two with two groups), whose cap, bias and
+//    exponential only it computes.
+//  * Values: A = the codes of V with the cache's rows as the contraction index, B = p * s -- p comes from the lane that has it with the
+//    multiplication itself -- rounded to bf16, the one rounding of the path beside the output's, for every (head, group).  A lane
+//    collects 8 rows' codes and regroups their halves.  What the 24 too many and z add does not depend on the channel: each lane sums
+//    p z - 24 (the rounded p s) in fp32.  Rows (channels) of the product and columns of another group belong to nobody.
 //  * A plain cache goes the same way without groups: columns are heads, values are regrouped halves.
 // A wave takes 32 rows at a time, the next ones on their way; its softmax has one reference per head that moves when a score is
-// 2^8 above it.  Weights: the scores go to the workspace as they come.
+// 2^8 above it.  The last rows are read as the last 32 of the cache, those before them masked (their scores are -inf; a row that holds NaN has
+// made the result NaN already), so that no read is clamped.  Weights: the scores go to the workspace as they come.
 #include "attn_decode_cache.h"
 
 namespace strd {
@@ -26,15 +28,17 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
+typedef float f32x2u __attribute__((ext_vector_type(2), aligned(4)));
 
 constexpr int kWaves = 4, kTrip = 32, kRound = kWaves * kTrip;
 constexpr float kLog2e = 1.4426950408889634f, kLazy = 8.f;
 
 __device__ __forceinline__ float ex2(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
-template <int N>
-__device__ __forceinline__ float row_ror(float v) {  // of the lane N places on in the row of 16, round its end
-    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x120 + N, 0xF, 0xF, true));
+template <int P0, int P1, int P2, int P3>
+__device__ __forceinline__ float quad(float v) {  // of lane P(its place) of this lane's quad
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), P0 | P1 << 2 | P2 << 4 | P3 << 6, 0xF, 0xF, true));
 }
 __device__ __forceinline__ float quarters_sum(float v) {
     v += __shfl_xor(v, 16, kWave);
@@ -65,10 +69,11 @@ struct Shape {
 };
 
 template <int D, bool KV4, int NP, bool BIAS>
-__global__ __launch_bounds__(kWaves *kWave) __attribute__((amdgpu_waves_per_eu(NP == 1 && !BIAS && (KV4 || D == 64) ? 3 : 2))) void decode_cache_mfma_kernel(
+__global__ __launch_bounds__(kWaves *kWave) __attribute__((amdgpu_waves_per_eu(NP == 1 && (KV4 || D == 64) ? 3 : 2))) void decode_cache_mfma_kernel(
     const bf16_t *__restrict__ q, CacheView cv, DecWs ws, int Tn, int Hq, int Hkv, int tps, int nsplit, ScoreMod mod) {
     using S = Shape<D, KV4>;
     constexpr int NG = S::kGroupsOfD, HP = S::kHeads, KS = S::kKSteps, VT = S::kVTiles, KD = S::kKDwords, VD = S::kVDwords;
+    constexpr int RL = 4 / NG;  // rows of a lane's four whose scores it ends up with
     __shared__ __attribute__((aligned(16))) float sm_o[kWaves][HP][D];
     __shared__ float sm_m[kWaves][HP], sm_l[kWaves][HP];
     int hk, split;
@@ -77,37 +82,41 @@ __global__ __launch_bounds__(kWaves *kWave) __attribute__((amdgpu_waves_per_eu(N
     const int rep = Hq / Hkv;
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int lr = lane & 15, c = lane >> 4;
-    const int grp = lr / HP, hcol = lr % HP;               // this lane's column: group of channels, head
-    const int kgrp = KV4 ? c * (D / 4) / kKv4Group : 0;    // group of the channels this lane holds of a key
-    const long long begin = (long long)split * tps;
-    const int t_end = (int)min((long long)Tn, begin + tps);
+    const int grp = lr % NG, hcol = lr / NG;             // this lane's column: head, group of channels
+    const int kgrp = KV4 ? c * (D / 4) / kKv4Group : 0;  // group of the channels this lane holds of a key
+    const int row_l = 4 * c + RL * grp;                  // first of its rows, of 16
+    const int begin = split * tps, t_end = min(Tn, begin + tps);
 
     struct Rows {
         uint32_t k[2][KD], v[8][VD], km[KV4 ? 8 : 1], vm[KV4 ? 8 : 1];
-        int32_t pos[BIAS ? 8 : 1];
+        int32_t pos[BIAS ? 2 : 1][RL];
     };
-    // Rows t0 .. t0 + 31 of this kv head; rows past the last one are read as that one, and masked.
-    const uint32_t k_stride = (uint32_t)Hkv * (KV4 ? D / 2 : D * 2), m_stride = (uint32_t)Hkv * (NG * 4);
-    auto load = [&](int t0, Rows &x) __attribute__((always_inline)) {
-        t0 = min(t0, Tn - 1);  // uniform
-        const int last = Tn - 1 - t0;
-        const char *kb = (const char *)cv.k + (size_t)t0 * k_stride + (size_t)hk * (k_stride / Hkv);
-        const char *vb = (const char *)cv.v + (size_t)t0 * k_stride + (size_t)hk * (k_stride / Hkv);
+    // 32 rows of this kv head from `base` on, all of them in the cache: a buffer of 32 rows for each side (whose size bounds every
+    // read), one offset a lane, and a uniform one for the row; no address is computed by a vector instruction.
+    const uint32_t kv_row = (uint32_t)Hkv * (KV4 ? D / 2 : D * 2), m_row = (uint32_t)Hkv * (NG * 4);
+    const uint32_t koff = hk * (KV4 ? D / 2 : D * 2) + lr * kv_row + (KV4 ? c * (D / 8) : 16 * c);
+    const uint32_t voff = hk * (KV4 ? D / 2 : D * 2) + 4 * c * kv_row + lr * (KV4 ? D / 32 : D / 8), moff = hk * (NG * 4) + 4 * c * m_row + 4 * grp;
+    auto rows_of = [&](const void *p, int base, uint32_t row) __attribute__((always_inline)) {
+        return __builtin_amdgcn_make_buffer_rsrc((char *)const_cast<void *>(p) + (size_t)base * row, (short)0, (int)(kTrip * row), 0x00027000);
+    };
+    auto load = [&](int base, Rows &x) __attribute__((always_inline)) {
+        const auto kb = rows_of(cv.k, base, kv_row), vb = rows_of(cv.v, base, kv_row);
+        const auto kmb = rows_of(cv.km, base, m_row), vmb = rows_of(cv.vm, base, m_row);
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const uint32_t off = (uint32_t)min(16 * u + lr, last) * k_stride;
+            const uint32_t at = 16 * u * kv_row;
             if constexpr (KV4 && D == 128) {
-                const u32x4 d = *reinterpret_cast<const u32x4 *>(kb + off + 16 * c);
+                const u32x4 d = __builtin_amdgcn_raw_buffer_load_b128(kb, koff, at, 0);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) x.k[u][i] = d[i];
             } else if constexpr (KV4) {
-                const u32x2 d = *reinterpret_cast<const u32x2 *>(kb + off + 8 * c);
+                const u32x2 d = __builtin_amdgcn_raw_buffer_load_b64(kb, koff, at, 0);
                 x.k[u][0] = d[0];
                 x.k[u][1] = d[1];
             } else {
 #pragma unroll
                 for (int i = 0; i < KS; ++i) {
-                    const u32x4 d = *reinterpret_cast<const u32x4 *>(kb + off + 64 * i + 16 * c);
+                    const u32x4 d = __builtin_amdgcn_raw_buffer_load_b128(kb, koff + 64 * i, at, 0);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) x.k[u][4 * i + e] = d[e];
                 }
@@ -115,36 +124,41 @@ __global__ __launch_bounds__(kWaves *kWave) __attribute__((amdgpu_waves_per_eu(N
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const uint32_t row = (uint32_t)min(16 * (e >> 2) + 4 * c + (e & 3), last);
-            const uint32_t off = row * k_stride;
+            const uint32_t row = 16 * (e >> 2) + (e & 3);
             if constexpr (KV4 && D == 128) {
-                x.v[e][0] = *reinterpret_cast<const uint32_t *>(vb + off + 4 * lr);
+                x.v[e][0] = __builtin_amdgcn_raw_buffer_load_b32(vb, voff, row * kv_row, 0);
             } else if constexpr (KV4) {
-                x.v[e][0] = *reinterpret_cast<const uint16_t *>(vb + off + 2 * lr);
+                x.v[e][0] = __builtin_amdgcn_raw_buffer_load_b16(vb, voff, row * kv_row, 0);
             } else if constexpr (D == 128) {
-                const u32x4 d = *reinterpret_cast<const u32x4 *>(vb + off + 16 * lr);
+                const u32x4 d = __builtin_amdgcn_raw_buffer_load_b128(vb, voff, row * kv_row, 0);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) x.v[e][i] = d[i];
             } else {
-                const u32x2 d = *reinterpret_cast<const u32x2 *>(vb + off + 8 * lr);
+                const u32x2 d = __builtin_amdgcn_raw_buffer_load_b64(vb, voff, row * kv_row, 0);
                 x.v[e][0] = d[0];
                 x.v[e][1] = d[1];
             }
             if constexpr (KV4) {
-                const uint32_t mo = row * m_stride + 4 * grp;
-                x.km[e] = *reinterpret_cast<const uint32_t *>((const char *)cv.km + ((size_t)t0 * Hkv + hk) * (NG * 4) + mo);
-                x.vm[e] = *reinterpret_cast<const uint32_t *>((const char *)cv.vm + ((size_t)t0 * Hkv + hk) * (NG * 4) + mo);
+                x.km[e] = __builtin_amdgcn_raw_buffer_load_b32(kmb, moff, row * m_row, 0);
+                x.vm[e] = __builtin_amdgcn_raw_buffer_load_b32(vmb, moff, row * m_row, 0);
             }
         }
         if constexpr (BIAS) {
-            if (mod.pos) {  // uniform
+            // (without positions a buffer of no bytes: reads that return 0 and are not looked at, but no branch, behind which every
+            // outstanding read would be waited for)
+            const auto pb = __builtin_amdgcn_make_buffer_rsrc((char *)const_cast<int32_t *>(mod.pos) + (mod.pos ? (size_t)base * 4 : 0), (short)0,
+                                                              mod.pos ? kTrip * 4 : 0, 0x00027000);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x.pos[e] = mod.pos[t0 + min(16 * (e >> 2) + 4 * c + (e & 3), last)];
-            }
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int k = 0; k < RL; ++k) x.pos[u][k] = __builtin_amdgcn_raw_buffer_load_b32(pb, 4 * row_l + 4 * k, 64 * u, 0);
         }
     };
+    Rows xa, xb;
+    const int t_first = begin + kTrip * wave;
+    load(min(t_first, Tn - kTrip), xa);
 
-    // the query heads: B operand, column (grp, hcol), k slots as the keys' codes come (the pairs of code_pair), zeros outside
+    // the query heads: B operand, column (hcol, grp), k slots as the keys' codes come (the pairs of code_pair), zeros outside
     // the column's group
     bf16x8 bq[NP][KS];
     float qsum[NP], slope[NP], m[NP], l[NP], corr[NP];
@@ -168,7 +182,7 @@ __global__ __launch_bounds__(kWaves *kWave) __attribute__((amdgpu_waves_per_eu(N
             if constexpr (KV4) z = mfma16(ones, bq[p][i], z);
         }
         qsum[p] = z[0];
-        slope[p] = BIAS && hh < rep ? mod.slopes[hk * rep + hh] : 0.f;
+        slope[p] = BIAS && hh < rep ? mod.slopes[hk * rep + hh] * kLog2e : 0.f;
         m[p] = kDecNegBig;
         l[p] = corr[p] = 0.f;
 #pragma unroll
@@ -176,11 +190,16 @@ __global__ __launch_bounds__(kWaves *kWave) __attribute__((amdgpu_waves_per_eu(N
     }
     float pos_q = 0.f;
     if constexpr (BIAS) pos_q = mod.pos ? (float)mod.pos[Tn - 1] : (float)(Tn - 1);
+    const size_t soff = (size_t)hcol * ws.ldt + row_l;
+    const bool capped = mod.cap > 0.f;  // uniform
+    const float dot_scale = capped ? mod.scale * mod.inv_cap : mod.scale * kLog2e, cap2 = mod.cap * kLog2e;
 
+    // the 32 rows from t0 on, in x those from min(t0, Tn - 32) on
     auto fold = [&](int t0, const Rows &x) __attribute__((always_inline)) {
-        const bool tail = t0 + kTrip > t_end;  // uniform
-        bf16x8 pb[NP];                         // p (4 bits: p * s of the column's group) of the 32 rows, the next product's operand
-        float pr[NP][2][4];
+        const int base = min(t0, Tn - kTrip);
+        const bool all = base == t0;  // uniform
+        bf16x8 pb[NP];                // p (4 bits: p * s of the column's group) of the 32 rows, the next product's operand
+        float pr[NP][2][RL];
         // ---- scores ----
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
@@ -192,73 +211,111 @@ __global__ __launch_bounds__(kWaves *kWave) __attribute__((amdgpu_waves_per_eu(N
                 else
                     ka[i] = __builtin_bit_cast(bf16x8, u32x4{x.k[u][4 * i], x.k[u][4 * i + 1], x.k[u][4 * i + 2], x.k[u][4 * i + 3]});
             }
-            float far[4];
-            if constexpr (BIAS) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) far[i] = fabsf(pos_q - (float)(mod.pos ? x.pos[4 * u + i] : t0 + 16 * u + 4 * c + i));
-            }
 #pragma unroll
             for (int p = 0; p < NP; ++p) {
-                f32x4 z = f32x4{0.f, 0.f, 0.f, 0.f};
+                const float start = KV4 ? -24.f * qsum[p] : 0.f;
+                f32x4 z = f32x4{start, start, start, start};
 #pragma unroll
                 for (int i = 0; i < KS; ++i) z = mfma16(ka[i], bq[p][i], z);
+                if constexpr (KV4) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float s = z[i];
-                    if constexpr (KV4) {
+                    for (int i = 0; i < 4; ++i) {
                         const Kv4Group g = kv4_meta(x.km[4 * u + i]);
-                        s = fmaf(g.s, s, fmaf(-24.f, g.s, g.z) * qsum[p]);
-                        s += row_ror<8>(s);
-                        if constexpr (NG == 4) s += row_ror<4>(s);
+                        z[i] = fmaf(g.s, z[i], g.z * qsum[p]);
                     }
-                    pr[p][u][i] = s * mod.scale;
+                }
+                // the groups' parts meet: a lane keeps its rows and hands the others on
+                if constexpr (NG == 4) {
+                    const bool hi = grp & 2, odd = grp & 1;
+                    float k0 = hi ? z[2] : z[0], k1 = hi ? z[3] : z[1];
+                    const float g0 = hi ? z[0] : z[2], g1 = hi ? z[1] : z[3];
+                    k0 += quad<2, 3, 0, 1>(g0);
+                    k1 += quad<2, 3, 0, 1>(g1);
+                    pr[p][u][0] = (odd ? k1 : k0) + quad<1, 0, 3, 2>(odd ? k0 : k1);
+                } else if constexpr (NG == 2) {
+                    const bool odd = grp & 1;
+                    pr[p][u][0] = (odd ? z[2] : z[0]) + quad<1, 0, 3, 2>(odd ? z[0] : z[2]);
+                    pr[p][u][1] = (odd ? z[3] : z[1]) + quad<1, 0, 3, 2>(odd ? z[1] : z[3]);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < RL; ++k) pr[p][u][k] = z[k];
                 }
             }
-            if (mod.cap > 0.f) {  // uniform
-                bool wide = false;
+        }
+#pragma unroll
+        for (int p = 0; p < NP; ++p)
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int k = 0; k < RL; ++k) pr[p][u][k] *= dot_scale;
+        if (capped) {
+            float far = 0.f;
+#pragma unroll
+            for (int p = 0; p < NP; ++p)
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int k = 0; k < RL; ++k) far = fmaxf(far, fabsf(pr[p][u][k]));
+            if (__any(far > 0.5f)) {
 #pragma unroll
                 for (int p = 0; p < NP; ++p)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        pr[p][u][i] *= mod.inv_cap;
-                        wide |= fabsf(pr[p][u][i]) > 0.5f;
-                    }
-                if (__any(wide)) {
+                    for (int u = 0; u < 2; ++u)
 #pragma unroll
-                    for (int p = 0; p < NP; ++p)
+                        for (int k = 0; k < RL; ++k) pr[p][u][k] = cap2 * tanhf(pr[p][u][k]);
+            } else {
+                // tanh(y) / y up to y = 0.5, as a polynomial in y^2 of least relative error (1.3e-8)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) pr[p][u][i] = mod.cap * tanhf(pr[p][u][i]);
-                } else {
-                    // tanh(y) / y up to y = 0.5, as a polynomial in y^2 of least relative error (1.3e-8)
+                for (int p = 0; p < NP; ++p)
 #pragma unroll
-                    for (int p = 0; p < NP; ++p)
+                    for (int u = 0; u < 2; ++u)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const float y = pr[p][u][i], w = y * y;
+                        for (int k = 0; k < RL; ++k) {
+                            const float y = pr[p][u][k], w = y * y;
                             float r = fmaf(w, 0.0171347708f, -0.0529858599f);
                             r = fmaf(w, r, 0.133247737f);
                             r = fmaf(w, r, -0.333330689f);
                             r = fmaf(w, r, 0.999999987f);
-                            pr[p][u][i] = mod.cap * (y * r);
+                            pr[p][u][k] = cap2 * y * r;
                         }
-                }
             }
+        }
+        if constexpr (BIAS) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int k = 0; k < RL; ++k) {
+                    const float far = fabsf(pos_q - (float)(mod.pos ? x.pos[u][k] : base + 16 * u + row_l + k));
+#pragma unroll
+                    for (int p = 0; p < NP; ++p) pr[p][u][k] = fmaf(-slope[p], far, pr[p][u][k]);
+                }
+        }
+        if (!all) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int k = 0; k < RL; ++k)
+#pragma unroll
+                    for (int p = 0; p < NP; ++p) pr[p][u][k] = base + 16 * u + row_l + k < t0 ? -INFINITY : pr[p][u][k];
+        }
+        if (ws.scores) {  // uniform
+            float *const sc = ws.scores + (size_t)(hk * rep) * ws.ldt + base;  // uniform
 #pragma unroll
             for (int p = 0; p < NP; ++p)
+                if (p * HP + hcol < rep)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float s = pr[p][u][i];
-                    if constexpr (BIAS) s = fmaf(-slope[p], far[i], s);
-                    s *= kLog2e;
-                    pr[p][u][i] = tail && t0 + 16 * u + 4 * c + i >= t_end ? -INFINITY : s;
-                }
-            if (ws.scores) {  // uniform; a head's four rows are one vector, from the lanes of its first group
+                    for (int u = 0; u < 2; ++u) {
+                        float *const at = sc + (size_t)(p * HP) * ws.ldt + 16 * u + soff;
+                        if (all) {
+                            if constexpr (RL == 4) *reinterpret_cast<f32x4u *>(at) = f32x4u{pr[p][u][0], pr[p][u][1], pr[p][u][2], pr[p][u][3]};
+                            else if constexpr (RL == 2) *reinterpret_cast<f32x2u *>(at) = f32x2u{pr[p][u][0], pr[p][u][1]};
+                            else at[0] = pr[p][u][0];
+                        } else {
 #pragma unroll
-                for (int p = 0; p < NP; ++p)
-                    if (grp == 0 && p * HP + hcol < rep && t0 + 16 * u + 4 * c < t_end)
-                        *reinterpret_cast<f32x4 *>(ws.scores + (size_t)(hk * rep + p * HP + hcol) * ws.ldt + t0 + 16 * u + 4 * c) =
-                            f32x4{pr[p][u][0], pr[p][u][1], pr[p][u][2], pr[p][u][3]};
-            }
+                            for (int k = 0; k < RL; ++k)
+                                if (base + 16 * u + row_l + k >= t0) at[k] = pr[p][u][k];
+                        }
+                    }
         }
         // ---- softmax ----
         float tm[NP];
@@ -269,13 +326,16 @@ __global__ __launch_bounds__(kWaves *kWave) __attribute__((amdgpu_waves_per_eu(N
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) tm[p] = fmaxf(tm[p], pr[p][u][i]);
+                for (int k = 0; k < RL; ++k) tm[p] = fmaxf(tm[p], pr[p][u][k]);
             moves |= tm[p] > m[p] + kLazy;
         }
         if (__any(moves)) {
 #pragma unroll
             for (int p = 0; p < NP; ++p) {
-                const float nm = fmaxf(m[p], quarters_max(tm[p])), f = ex2(m[p] - nm);
+                float t = tm[p];
+                if constexpr (NG >= 2) t = fmaxf(t, quad<1, 0, 3, 2>(t));
+                if constexpr (NG == 4) t = fmaxf(t, quad<2, 3, 0, 1>(t));
+                const float nm = fmaxf(m[p], quarters_max(t)), f = ex2(m[p] - nm);
                 m[p] = nm;
                 l[p] *= f;
                 corr[p] *= f;
@@ -288,19 +348,30 @@ __global__ __launch_bounds__(kWaves *kWave) __attribute__((amdgpu_waves_per_eu(N
             uint32_t w[4];
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                float ps[4];
+                float e[RL], ps[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float e = ex2(pr[p][u][i] - m[p]);
-                    l[p] += e;
-                    ps[i] = e;
-                    if constexpr (KV4) {
-                        const Kv4Group g = kv4_meta(x.vm[4 * u + i]);
-                        const bool out = tail && t0 + 16 * u + 4 * c + i >= t_end;  // (a group behind the last row may hold NaN)
-                        ps[i] = out ? 0.f : e * g.s;
-                        corr[p] = out ? corr[p] : fmaf(e, g.z, corr[p]);
-                    }
+                for (int k = 0; k < RL; ++k) {
+                    e[k] = ex2(pr[p][u][k] - m[p]);
+                    l[p] += e[k];
                 }
+                auto of_row = [&](auto ic) __attribute__((always_inline)) {
+                    constexpr int I = decltype(ic)::value;
+                    float pi;
+                    if constexpr (NG == 4) pi = quad<I, I, I, I>(e[0]);
+                    else if constexpr (NG == 2) pi = quad<I / 2, I / 2, 2 + I / 2, 2 + I / 2>(e[I % 2]);
+                    else pi = e[I % RL];
+                    if constexpr (KV4) {
+                        const Kv4Group g = kv4_meta(x.vm[4 * u + I]);
+                        ps[I] = pi * g.s;
+                        corr[p] = fmaf(pi, g.z, corr[p]);
+                    } else {
+                        ps[I] = pi;
+                    }
+                };
+                of_row(std::integral_constant<int, 0>());
+                of_row(std::integral_constant<int, 1>());
+                of_row(std::integral_constant<int, 2>());
+                of_row(std::integral_constant<int, 3>());
                 w[2 * u] = bf16_pair(ps[0], ps[1]);
                 w[2 * u + 1] = bf16_pair(ps[2], ps[3]);
             }
@@ -315,19 +386,19 @@ __global__ __launch_bounds__(kWaves *kWave) __attribute__((amdgpu_waves_per_eu(N
         // halves of two rows' dwords side by side: lo of both, hi of both
         auto pair_lo = [](uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); };
         auto pair_hi = [](uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); };
-        uint32_t va[8][VD];
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-#pragma unroll
-            for (int i = 0; i < VD; ++i)
-                va[e][i] = !KV4 && tail && t0 + 16 * (e >> 2) + 4 * c + (e & 3) >= t_end ? 0u : x.v[e][i];  // (0 times what is not finite)
         uint32_t lo[4][VD], hi[4][VD];
 #pragma unroll
         for (int e = 0; e < 4; ++e)
 #pragma unroll
             for (int i = 0; i < VD; ++i) {
-                lo[e][i] = pair_lo(va[2 * e][i], va[2 * e + 1][i]);
-                hi[e][i] = pair_hi(va[2 * e][i], va[2 * e + 1][i]);
+                uint32_t a = x.v[2 * e][i], b = x.v[2 * e + 1][i];
+                if (!KV4 && !all) {  // (a probability of 0 times what is not finite)
+                    const int row = base + 16 * (e >> 1) + 4 * c + 2 * (e & 1);
+                    a = row < t0 ? 0u : a;
+                    b = row + 1 < t0 ? 0u : b;
+                }
+                lo[e][i] = pair_lo(a, b);
+                hi[e][i] = pair_hi(a, b);
             }
         auto product = [&](auto jc) __attribute__((always_inline)) {
             constexpr int J = decltype(jc)::value;
@@ -354,18 +425,11 @@ __global__ __launch_bounds__(kWaves *kWave) __attribute__((amdgpu_waves_per_eu(N
         product(std::integral_constant<int, 7>());
     };
 
-    {
-        Rows a, b;
-        int t0 = (int)min(begin + kTrip * wave, (long long)Tn);
-        load(t0, a);
-        for (; t0 < t_end; t0 += 2 * kRound) {
-            load(min(t0 + kRound, Tn), b);
-            fold(t0, a);
-            if (t0 + kRound < t_end) {
-                load(min(t0 + 2 * kRound, Tn), a);
-                fold(t0 + kRound, b);
-            }
-        }
+    for (int t0 = t_first; t0 < t_end; t0 += 2 * kRound) {
+        load(min(t0 + kRound, Tn - kTrip), xb);
+        fold(t0, xa);
+        load(min(t0 + 2 * kRound, Tn - kTrip), xa);
+        if (t0 + kRound < t_end) fold(t0 + kRound, xb);
     }
 
     // ---- the four waves join, one set of heads at a time ----
@@ -374,6 +438,8 @@ __global__ __launch_bounds__(kWaves *kWave) __attribute__((amdgpu_waves_per_eu(N
         const int nh = min(HP, rep - p * HP);
         if (nh <= 0) break;  // uniform
         if (p) __syncthreads();
+        if constexpr (NG >= 2) l[p] += quad<1, 0, 3, 2>(l[p]);
+        if constexpr (NG == 4) l[p] += quad<2, 3, 0, 1>(l[p]);
         l[p] = quarters_sum(l[p]);
         corr[p] = quarters_sum(corr[p]);
         // rows 4 c + i of product j are channels VT (4 c + i) + j; a lane's column counts for its own group's channels
@@ -385,7 +451,7 @@ __global__ __launch_bounds__(kWaves *kWave) __attribute__((amdgpu_waves_per_eu(N
                     *reinterpret_cast<f32x4 *>(&sm_o[wave][hcol][VT * (4 * c + i) + j]) =
                         f32x4{oacc[p][j][i] + corr[p], oacc[p][j + 1][i] + corr[p], oacc[p][j + 2][i] + corr[p], oacc[p][j + 3][i] + corr[p]};
         }
-        if (lane < HP) {
+        if (c == 0 && grp == 0) {
             sm_m[wave][hcol] = m[p];
             sm_l[wave][hcol] = l[p];
         }
@@ -422,9 +488,10 @@ void launch_bias(const DecCall &a, const DecWs &ws, int nsplit, int tps, hipStre
 
 }  // namespace
 
-// Rows are read at 32-bit offsets from the first of 32: any that fit a GPU's memory.
-bool dec_mfma_supported(int Hq, int Hkv, int d, bool kv4, strd_dtype io) {
-    if (io != STRD_BF16 || (d != 64 && d != 128) || Hkv > 8192) return false;
+// 32 rows are read at a time, at 32-bit offsets from the first: caches of 32 rows at least (fewer: the launches' latency, whatever
+// is launched), of up to 8192 heads.
+bool dec_mfma_supported(int T, int Hq, int Hkv, int d, bool kv4, strd_dtype io) {
+    if (T < kTrip || io != STRD_BF16 || (d != 64 && d != 128) || Hkv > 8192) return false;
     const int rep = Hq / Hkv;
     return rep <= (kv4 && d == 128 ? 8 : 16);
 }
