@@ -56,8 +56,8 @@ __device__ __forceinline__ void dec_place(int b, int Hkv, int &hk, int &split) {
 inline int dec_grid(int Hkv, int nsplit) { return Hkv * ((nsplit + kXcd - 1) / kXcd * kXcd); }
 
 bool dec_mfma_supported(int T, int Hq, int Hkv, int d, bool kv4, strd_dtype io);
-int dec_mfma_splits(int T, int Hkv, int &tps);
-void dec_mfma(const DecCall &a, const DecWs &ws, int nsplit, int tps, hipStream_t st);
+int dec_mfma_splits(int T, int Hkv, int d, bool kv4, int &tps);
+int dec_mfma(const DecCall &a, const DecWs &ws, int nsplit, int tps, hipStream_t st);
 int dec_splits_general(int T, int Hq, int Hkv, int &tps);
 int dec_combine(const DecCall &a, const DecWs &ws, int nsplit, hipStream_t st);
 

@@ -333,7 +333,7 @@ int dec_combine(const DecCall &a, const DecWs &ws, int nsplit, hipStream_t st) {
 size_t attn_decode_cache_ws(int T, int Hq, int Hkv, int d, bool kv4, bool weights, strd_dtype io) {
     // (a plain cache that 16-byte reads do not fit takes the general kernel whatever its shape: room for either's splits)
     int tps, n = dec_splits_general(T, Hq, Hkv, tps);
-    if (dec_mfma_supported(T, Hq, Hkv, d, kv4, io)) n = kv4 ? dec_mfma_splits(T, Hkv, tps) : max(n, dec_mfma_splits(T, Hkv, tps));
+    if (dec_mfma_supported(T, Hq, Hkv, d, kv4, io)) n = kv4 ? dec_mfma_splits(T, Hkv, d, kv4, tps) : max(n, dec_mfma_splits(T, Hkv, d, kv4, tps));
     return dec_ws_bytes(n, Hq, d, dec_ldt(T), weights);
 }
 
@@ -341,13 +341,15 @@ int attn_decode_cache(const DecCall &a, void *wsp, hipStream_t st) {
     const bool mfma = dec_mfma_supported(a.T, a.Hq, a.Hkv, a.d, a.kv4, a.io) && (((uintptr_t)a.q | (uintptr_t)a.c.k | (uintptr_t)a.c.v) & 15) == 0;
     DecWs ws;
     int tps;
-    const int nsplit = mfma ? dec_mfma_splits(a.T, a.Hkv, tps) : dec_splits_general(a.T, a.Hq, a.Hkv, tps);
+    const int nsplit = mfma ? dec_mfma_splits(a.T, a.Hkv, a.d, a.kv4, tps) : dec_splits_general(a.T, a.Hq, a.Hkv, tps);
     ws.ml = (float *)wsp;  // (pairs: they come first)
     ws.part = ws.ml + (size_t)nsplit * a.Hq * 2;
     ws.ldt = dec_ldt(a.T);
     ws.scores = a.w_out ? (float *)((char *)wsp + align_up((size_t)nsplit * a.Hq * (a.d + 2) * sizeof(float), 256)) : nullptr;
-    if (mfma) dec_mfma(a, ws, nsplit, tps, st);
-    else if (a.io == STRD_BF16) launch_typed<bf16_t>(a, ws, nsplit, tps, st);
+    if (mfma) {
+        const int rc = dec_mfma(a, ws, nsplit, tps, st);
+        if (rc != STRD_OK) return rc;
+    } else if (a.io == STRD_BF16) launch_typed<bf16_t>(a, ws, nsplit, tps, st);
     else launch_typed<float>(a, ws, nsplit, tps, st);
     if (hipGetLastError() != hipSuccess) return STRD_EHIP;
     return dec_combine(a, ws, nsplit, st);

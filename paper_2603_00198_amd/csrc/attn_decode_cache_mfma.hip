@@ -31,7 +31,7 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
 typedef float f32x2u __attribute__((ext_vector_type(2), aligned(4)));
 
-constexpr int kWaves = 4, kTrip = 32, kRound = kWaves * kTrip;
+constexpr int kTrip = 32;
 constexpr float kLog2e = 1.4426950408889634f, kLazy = 8.f;
 
 __device__ __forceinline__ float ex2(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -51,12 +51,18 @@ __device__ __forceinline__ float quarters_max(float v) {
 __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
     return __builtin_bit_cast(uint32_t, bf16x2{(bf16_t)lo, (bf16_t)hi});
 }
-// Codes at bits 4 J and 16 + 4 J as a pair of bf16 numbers 16 + n: n belongs at bits 3 .. 6 of each half.
-template <int J>
-__device__ __forceinline__ uint32_t code_pair(uint32_t x) {
-    const uint32_t y = J == 0 ? x << 3 : x >> (4 * J - 3);
-    return (y & 0x00780078u) | 0x41804180u;
-}
+// Codes at bits 4 J and 16 + 4 J as a pair of bf16 numbers 16 + n: n belongs at bits 3 .. 6 of each half.  A bit-field insert into
+// a register whose value the compiler does not know -- with a constant it comes out as an and and an or.  (The statement that hides it
+// holds no instruction: one in inline assembly that writes a vector register is not kept apart from a matrix product's late write.)
+struct CodeBits {
+    uint32_t sixteen = 0x41804180u;
+    __device__ __forceinline__ CodeBits() { asm("" : "+v"(sixteen)); }
+    template <int J>
+    __device__ __forceinline__ uint32_t pair(uint32_t x) const {
+        constexpr uint32_t kMask = 0x00780078u;
+        return ((J == 0 ? x << 3 : x >> (4 * J - 3)) & kMask) | (sixteen & ~kMask);
+    }
+};
 
 template <int D, bool KV4>
 struct Shape {
@@ -68,23 +74,34 @@ struct Shape {
     static constexpr int kVDwords = KV4 ? 1 : D / 32;      // of a lane, per row (4 bits, D = 64: half of one)
 };
 
-template <int D, bool KV4, int NP, bool BIAS>
-__global__ __launch_bounds__(kWaves *kWave) __attribute__((amdgpu_waves_per_eu(NP == 1 && (KV4 || D == 64) ? 3 : 2))) void decode_cache_mfma_kernel(
-    const bf16_t *__restrict__ q, CacheView cv, DecWs ws, int Tn, int Hq, int Hkv, int tps, int nsplit, ScoreMod mod) {
+// Long caches, from about 16 MB on: a workgroup is as many waves as a CU holds of them (three on a SIMD, or two), on `hw` neighbouring
+// kv heads and the same rows: what heads share of a line of the cache -- two heads' codes, eight heads' (s, z) -- one CU fetches once.
+// Shorter ones: four waves on one kv head, which start and join sooner.  us of a step with four waves / as many as fit: 8 heads of 128 in 4 bits,
+// 843 rows 12.1 / 14.9, 6000 (8 MB) 15.9 / 16.9, 12000 (15 MB) 19.5 / 19.2, 131627 64.3 / 59.5; plain, 2500 (10 MB) 14.4 / 17.5, 6000
+// (25 MB) 21.4 / 18.6, 131627 143 / 127; 4 heads of 64 in 4 bits, 50000 (16 MB) 21.2 / 21.2; plain, 12000 (12 MB) 16.6 / 17.3.
+template <int D, bool KV4, int NP>
+constexpr int dec_waves() { return NP == 1 && (KV4 || D == 64) ? 12 : 8; }
+inline bool dec_long(int T, int Hkv, int d, bool kv4) { return (long long)T * Hkv * d * (kv4 ? 10 : 32) >= 8LL << 24; }
+inline int dec_heads(int T, int Hkv, int d, bool kv4) { return !dec_long(T, Hkv, d, kv4) ? 1 : Hkv % 4 == 0 ? 4 : Hkv % 2 == 0 ? 2 : 1; }
+
+template <int D, bool KV4, int NP, bool BIAS, int kWaves>
+__global__ __launch_bounds__(kWaves * kWave) __attribute__((amdgpu_waves_per_eu(NP == 1 && (KV4 || D == 64) ? 3 : 2))) void decode_cache_mfma_kernel(
+    const bf16_t *__restrict__ q, CacheView cv, DecWs ws, int Tn, int Hq, int Hkv, int hw, int tps, int nsplit, ScoreMod mod) {
     using S = Shape<D, KV4>;
     constexpr int NG = S::kGroupsOfD, HP = S::kHeads, KS = S::kKSteps, VT = S::kVTiles, KD = S::kKDwords, VD = S::kVDwords;
     constexpr int RL = 4 / NG;  // rows of a lane's four whose scores it ends up with
-    __shared__ __attribute__((aligned(16))) float sm_o[kWaves][HP][D];
-    __shared__ float sm_m[kWaves][HP], sm_l[kWaves][HP];
-    int hk, split;
-    dec_place(blockIdx.x, Hkv, hk, split);
+    extern __shared__ __attribute__((aligned(16))) float sm[];  // [kWaves][hs][D] values, [kWaves][hs] references and sums
+    int hg, split;
+    dec_place(blockIdx.x, Hkv / hw, hg, split);
     if (split >= nsplit) return;  // uniform
-    const int rep = Hq / Hkv;
+    const int rep = Hq / Hkv, hs = min(HP, rep);
+    float *const sm_m = sm + kWaves * hs * D, *const sm_l = sm_m + kWaves * hs;
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int hk = hg * hw + wave % hw, round = kWaves / hw * kTrip;  // this wave's kv head; rows of all waves' trips
     const int lr = lane & 15, c = lane >> 4;
     const int grp = lr % NG, hcol = lr / NG;             // this lane's column: head, group of channels
     const int kgrp = KV4 ? c * (D / 4) / kKv4Group : 0;  // group of the channels this lane holds of a key
-    const int row_l = 4 * c + RL * grp;                  // first of its rows, of 16
+    const int row_l = 4 * c + RL * grp;                   // first of its rows, of 16
     const int begin = split * tps, t_end = min(Tn, begin + tps);
 
     struct Rows {
@@ -155,10 +172,11 @@ __global__ __launch_bounds__(kWaves *kWave) __attribute__((amdgpu_waves_per_eu(N
         }
     };
     Rows xa, xb;
-    const int t_first = begin + kTrip * wave;
+    const CodeBits bits;
+    const int t_first = begin + kTrip * (wave / hw);
     load(min(t_first, Tn - kTrip), xa);
 
-    // the query heads: B operand, column (hcol, grp), k slots as the keys' codes come (the pairs of code_pair), zeros outside
+    // the query heads: B operand, column (hcol, grp), k slots as the keys' codes come (the pairs of CodeBits), zeros outside
     // the column's group
     bf16x8 bq[NP][KS];
     float qsum[NP], slope[NP], m[NP], l[NP], corr[NP];
@@ -207,7 +225,7 @@ __global__ __launch_bounds__(kWaves *kWave) __attribute__((amdgpu_waves_per_eu(N
 #pragma unroll
             for (int i = 0; i < KS; ++i) {
                 if constexpr (KV4)
-                    ka[i] = __builtin_bit_cast(bf16x8, u32x4{code_pair<0>(x.k[u][i]), code_pair<1>(x.k[u][i]), code_pair<2>(x.k[u][i]), code_pair<3>(x.k[u][i])});
+                    ka[i] = __builtin_bit_cast(bf16x8, u32x4{bits.pair<0>(x.k[u][i]), bits.pair<1>(x.k[u][i]), bits.pair<2>(x.k[u][i]), bits.pair<3>(x.k[u][i])});
                 else
                     ka[i] = __builtin_bit_cast(bf16x8, u32x4{x.k[u][4 * i], x.k[u][4 * i + 1], x.k[u][4 * i + 2], x.k[u][4 * i + 3]});
             }
@@ -407,7 +425,7 @@ __global__ __launch_bounds__(kWaves *kWave) __attribute__((amdgpu_waves_per_eu(N
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     if constexpr (KV4)
-                        a[e] = code_pair<J % 4>(J < 4 ? lo[e][0] : hi[e][0]);
+                        a[e] = bits.template pair<J % 4>(J < 4 ? lo[e][0] : hi[e][0]);
                     else
                         a[e] = J % 2 ? hi[e][J / 2] : lo[e][J / 2];
                 }
@@ -425,14 +443,14 @@ __global__ __launch_bounds__(kWaves *kWave) __attribute__((amdgpu_waves_per_eu(N
         product(std::integral_constant<int, 7>());
     };
 
-    for (int t0 = t_first; t0 < t_end; t0 += 2 * kRound) {
-        load(min(t0 + kRound, Tn - kTrip), xb);
+    for (int t0 = t_first; t0 < t_end; t0 += 2 * round) {
+        load(min(t0 + round, Tn - kTrip), xb);
         fold(t0, xa);
-        load(min(t0 + 2 * kRound, Tn - kTrip), xa);
-        if (t0 + kRound < t_end) fold(t0 + kRound, xb);
+        load(min(t0 + 2 * round, Tn - kTrip), xa);
+        if (t0 + round < t_end) fold(t0 + round, xb);
     }
 
-    // ---- the four waves join, one set of heads at a time ----
+    // ---- the waves of a kv head join, one set of query heads at a time ----
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
         const int nh = min(HP, rep - p * HP);
@@ -443,31 +461,29 @@ __global__ __launch_bounds__(kWaves *kWave) __attribute__((amdgpu_waves_per_eu(N
         l[p] = quarters_sum(l[p]);
         corr[p] = quarters_sum(corr[p]);
         // rows 4 c + i of product j are channels VT (4 c + i) + j; a lane's column counts for its own group's channels
-        if (!KV4 || grp == VT * 4 * c / kKv4Group) {
+        if (hcol < nh && (!KV4 || grp == VT * 4 * c / kKv4Group)) {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int j = 0; j < VT; j += 4)
-                    *reinterpret_cast<f32x4 *>(&sm_o[wave][hcol][VT * (4 * c + i) + j]) =
+                    *reinterpret_cast<f32x4 *>(sm + (wave * hs + hcol) * D + VT * (4 * c + i) + j) =
                         f32x4{oacc[p][j][i] + corr[p], oacc[p][j + 1][i] + corr[p], oacc[p][j + 2][i] + corr[p], oacc[p][j + 3][i] + corr[p]};
         }
-        if (c == 0 && grp == 0) {
-            sm_m[wave][hcol] = m[p];
-            sm_l[wave][hcol] = l[p];
+        if (c == 0 && grp == 0 && hcol < nh) {
+            sm_m[wave * hs + hcol] = m[p];
+            sm_l[wave * hs + hcol] = l[p];
         }
         __syncthreads();
-        for (int e = threadIdx.x; e < nh * D; e += kWaves * kWave) {
-            const int r = e / D, ch = e % D;
-            float mx = sm_m[0][r], num = 0.f, den = 0.f;
-#pragma unroll
-            for (int w = 1; w < kWaves; ++w) mx = fmaxf(mx, sm_m[w][r]);
-#pragma unroll
-            for (int w = 0; w < kWaves; ++w) {
-                const float f = ex2(sm_m[w][r] - mx);
-                num = fmaf(f, sm_o[w][r][ch], num);
-                den = fmaf(f, sm_l[w][r], den);
+        for (int e = threadIdx.x; e < hw * nh * D; e += kWaves * kWave) {
+            const int r = e / D % nh, ch = e % D, hl = e / (D * nh);
+            float mx = kDecNegBig, num = 0.f, den = 0.f;
+            for (int w = hl; w < kWaves; w += hw) mx = fmaxf(mx, sm_m[w * hs + r]);
+            for (int w = hl; w < kWaves; w += hw) {
+                const float f = ex2(sm_m[w * hs + r] - mx);
+                num = fmaf(f, sm[(w * hs + r) * D + ch], num);
+                den = fmaf(f, sm_l[w * hs + r], den);
             }
-            const size_t ph = (size_t)split * Hq + hk * rep + p * HP + r;
+            const size_t ph = (size_t)split * Hq + (hg * hw + hl) * rep + p * HP + r;
             ws.part[ph * D + ch] = num;
             if (ch == 0) {
                 ws.ml[2 * ph] = mx;
@@ -477,13 +493,21 @@ __global__ __launch_bounds__(kWaves *kWave) __attribute__((amdgpu_waves_per_eu(N
     }
 }
 
+template <int D, bool KV4, int NP, int kWaves>
+int launch_waves(const DecCall &a, const DecWs &ws, int nsplit, int tps, hipStream_t st) {
+    const int hw = dec_heads(a.T, a.Hkv, D, KV4), grid = dec_grid(a.Hkv / hw, nsplit), hs = min(Shape<D, KV4>::kHeads, a.Hq / a.Hkv);
+    const size_t smem = (size_t)kWaves * hs * (D + 2) * sizeof(float);
+    auto launch = [&](auto kernel) {
+        if (smem > 65536 && !allow_dynamic_lds(reinterpret_cast<const void *>(kernel), (size_t)kWaves * Shape<D, KV4>::kHeads * (D + 2) * sizeof(float)))
+            return (int)STRD_EHIP;
+        kernel<<<grid, kWaves * kWave, smem, st>>>((const bf16_t *)a.q, a.c, ws, a.T, a.Hq, a.Hkv, hw, tps, nsplit, a.mod);
+        return launch_status();
+    };
+    return a.mod.slopes ? launch(&decode_cache_mfma_kernel<D, KV4, NP, true, kWaves>) : launch(&decode_cache_mfma_kernel<D, KV4, NP, false, kWaves>);
+}
 template <int D, bool KV4, int NP>
-void launch_bias(const DecCall &a, const DecWs &ws, int nsplit, int tps, hipStream_t st) {
-    const int grid = dec_grid(a.Hkv, nsplit);
-    if (a.mod.slopes)
-        decode_cache_mfma_kernel<D, KV4, NP, true><<<grid, kWaves * kWave, 0, st>>>((const bf16_t *)a.q, a.c, ws, a.T, a.Hq, a.Hkv, tps, nsplit, a.mod);
-    else
-        decode_cache_mfma_kernel<D, KV4, NP, false><<<grid, kWaves * kWave, 0, st>>>((const bf16_t *)a.q, a.c, ws, a.T, a.Hq, a.Hkv, tps, nsplit, a.mod);
+int launch_bias(const DecCall &a, const DecWs &ws, int nsplit, int tps, hipStream_t st) {
+    return dec_long(a.T, a.Hkv, D, KV4) ? launch_waves<D, KV4, NP, dec_waves<D, KV4, NP>()>(a, ws, nsplit, tps, st) : launch_waves<D, KV4, NP, 4>(a, ws, nsplit, tps, st);
 }
 
 }  // namespace
@@ -496,27 +520,21 @@ bool dec_mfma_supported(int T, int Hq, int Hkv, int d, bool kv4, strd_dtype io) 
     return rep <= (kv4 && d == 128 ? 8 : 16);
 }
 
-// About 768 workgroups -- three on every CU, what their registers allow -- and 32 rows for each of their waves at least.
-int dec_mfma_splits(int T, int Hkv, int &tps) {
-    const int want = min(kDecMaxSplits, max(1, 768 / Hkv));
-    tps = (int)(((long long)ceil_div(T, want) + kRound - 1) / kRound * kRound);
+// Long: a workgroup on every CU.  Short: a trip for each of the four waves, up to three workgroups on every CU.
+int dec_mfma_splits(int T, int Hkv, int d, bool kv4, int &tps) {
+    const bool longer = dec_long(T, Hkv, d, kv4);
+    const int hw = dec_heads(T, Hkv, d, kv4), round = (longer ? 12 / hw : 4) * kTrip;
+    const int want = min(kDecMaxSplits, max(1, (longer ? 256 * hw : 768) / Hkv));
+    tps = (int)(((long long)ceil_div(T, want) + round - 1) / round * round);
     return (int)(((long long)T + tps - 1) / tps);
 }
 
-void dec_mfma(const DecCall &a, const DecWs &ws, int nsplit, int tps, hipStream_t st) {
+int dec_mfma(const DecCall &a, const DecWs &ws, int nsplit, int tps, hipStream_t st) {
     const int rep = a.Hq / a.Hkv;
-    if (a.kv4) {
-        if (a.d == 128) {
-            if (rep <= 4) launch_bias<128, true, 1>(a, ws, nsplit, tps, st);
-            else launch_bias<128, true, 2>(a, ws, nsplit, tps, st);
-        } else {
-            if (rep <= 8) launch_bias<64, true, 1>(a, ws, nsplit, tps, st);
-            else launch_bias<64, true, 2>(a, ws, nsplit, tps, st);
-        }
-    } else {
-        if (a.d == 128) launch_bias<128, false, 1>(a, ws, nsplit, tps, st);
-        else launch_bias<64, false, 1>(a, ws, nsplit, tps, st);
-    }
+    if (a.kv4 && a.d == 128)
+        return rep <= 4 ? launch_bias<128, true, 1>(a, ws, nsplit, tps, st) : launch_bias<128, true, 2>(a, ws, nsplit, tps, st);
+    if (a.kv4) return rep <= 8 ? launch_bias<64, true, 1>(a, ws, nsplit, tps, st) : launch_bias<64, true, 2>(a, ws, nsplit, tps, st);
+    return a.d == 128 ? launch_bias<128, false, 1>(a, ws, nsplit, tps, st) : launch_bias<64, false, 1>(a, ws, nsplit, tps, st);
 }
 
 }  // namespace strd
