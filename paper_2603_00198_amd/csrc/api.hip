@@ -501,6 +501,8 @@ int strd_attn_decode_step(const void *q, const void *k_cache, const void *v_cach
 // ------------------------------------------------------------------ packed attention, caches -
 namespace {
 inline bool cap_ok(float cap) { return cap >= 0.f && cap < INFINITY; }
+// Within the range where cap * log2 e and 1 / cap are numbers: a score under 1e30 is the same with either cap, and so is one capped to nothing.
+inline float cap_in_range(float cap) { return cap > 0.f ? std::min(std::max(cap, 1e-30f), 1e30f) : 0.f; }
 
 int decode_cache_call(DecCall &a, float scale, float cap, const float *slopes, const int32_t *pos, void *ws, size_t ws_bytes, void *stream) {
     if (a.T < 1 || a.T > kMostRows || a.Hq < 1 || a.Hkv < 1 || a.d < 1 || a.Hq % a.Hkv || !io_ok(a.io) || !(scale > 0.f) || !cap_ok(cap) || !a.q ||
@@ -510,6 +512,7 @@ int decode_cache_call(DecCall &a, float scale, float cap, const float *slopes, c
     if (a.kv4 && !aligned16(a.c.k, a.c.km, a.c.v, a.c.vm)) return STRD_EINVAL;
     const size_t need = attn_decode_cache_ws(a.T, a.Hq, a.Hkv, a.d, a.kv4, a.w_out != nullptr, a.io);
     if (!ws || ws_bytes < need || !aligned16(ws)) return STRD_EWORKSPACE;
+    cap = cap_in_range(cap);
     a.mod = {scale, cap, cap > 0.f ? 1.f / cap : 0.f, slopes, pos};
     return attn_decode_cache(a, ws, as_stream(stream));
 }
@@ -531,6 +534,7 @@ int strd_attn_prefill_varlen(const void *q, int64_t ldq, const void *k, int64_t 
         return STRD_EINVAL;
     if (rows == 0) return STRD_OK;
     m.ldq = ldq, m.ldk = ldk, m.ldv = ldv;
+    cap = cap_in_range(cap);
     m.scale = scale, m.cap = cap, m.inv_cap = cap > 0.f ? 1.f / cap : 0.f;
     m.slopes = slopes, m.pos = pos, m.prefix = prefix != 0;
     if (!attn_general_supported(d)) return STRD_EUNSUPPORTED;

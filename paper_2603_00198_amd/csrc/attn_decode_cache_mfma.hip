@@ -173,8 +173,10 @@ __global__ __launch_bounds__(kWaves * kWave) __attribute__((amdgpu_waves_per_eu(
     };
     Rows xa, xb;
     const CodeBits bits;
-    const int t_first = begin + kTrip * (wave / hw);
-    load(min(t_first, Tn - kTrip), xa);
+    // trips from the last to the first: with a bias from far to near the softmax reference would move in every one
+    const int t_first = begin + kTrip * (wave / hw), trips = t_first < t_end ? (t_end - t_first + round - 1) / round : 0;
+    auto trip_at = [&](int i) { return t_first + max(trips - 1 - i, 0) * round; };
+    load(min(trip_at(0), Tn - kTrip), xa);
 
     // the query heads: B operand, column (hcol, grp), k slots as the keys' codes come (the pairs of CodeBits), zeros outside
     // the column's group
@@ -443,11 +445,11 @@ __global__ __launch_bounds__(kWaves * kWave) __attribute__((amdgpu_waves_per_eu(
         product(std::integral_constant<int, 7>());
     };
 
-    for (int t0 = t_first; t0 < t_end; t0 += 2 * round) {
-        load(min(t0 + round, Tn - kTrip), xb);
-        fold(t0, xa);
-        load(min(t0 + 2 * round, Tn - kTrip), xa);
-        if (t0 + round < t_end) fold(t0 + round, xb);
+    for (int i = 0; i < trips; i += 2) {
+        load(min(trip_at(i + 1), Tn - kTrip), xb);
+        fold(trip_at(i), xa);
+        load(min(trip_at(i + 2), Tn - kTrip), xa);
+        if (i + 1 < trips) fold(trip_at(i + 1), xb);
     }
 
     // ---- the waves of a kv head join, one set of query heads at a time ----

@@ -4,9 +4,9 @@
 //  * Blocks are dealt by level over the sequences (AttnTab), the longest first; rows have pitches.
 //  * A row sees the keys before its limit: its own number + 1, or its sequence's vision rows.  Limits never fall from one row to
 //    the next, so a wave meets at most two 32-key blocks that only some of its rows see.
-//  * A score becomes cap * tanh(score / cap) as c - 2 c / (2^(score * 2 log2 e / cap) + 1), in units of log2 e: two transcendental
-//    instructions of a quarter's rate beside the softmax's one.  The bias takes the rows' positions from LDS, where they lie as fp32
-//    numbers beside the keys.
+//  * A score becomes cap * tanh(score / cap): where the scores of a block are up to cap / 2, a polynomial in the square (five
+//    instructions), else c - 2 c / (2^(score * 2 log2 e / cap) + 1) in units of log2 e, with two transcendental instructions of a quarter's
+//    rate beside the softmax's one.  The bias takes the rows' positions from LDS, where they lie as fp32 numbers beside the keys.
 //  * What a row does not see does not reach it.  A probability of 0 takes a value out of the second product only if it is finite: in
 //    chunks with hidden keys the values are looked at when they have landed in LDS, and those that are not finite are taken out and
 //    added at the end, row by row.  And a row's softmax reference moves by the row's own scores alone, never because of a neighbour in its wave: a row's
@@ -78,7 +78,9 @@ struct Params {
     const bf16_t *q, *k, *v;
     bf16_t *o;
     int Hq, Hkv, xcd_map;
-    float scale2, kappa, c2;  // scale * log2 e; 2 log2 e * scale / cap, cap * log2 e
+    float scale2;              // scale * log2 e
+    float near, kappa, c2, c2_twice;  // with a cap: raw scores up to which the polynomial holds, 2 log2 e * scale / cap, cap * log2 e, -2 cap * log2 e
+    float tanh[4];             // cap log2 e tanh(raw scale / cap) / raw in powers of raw^2
     AttnMod mod;
 };
 
@@ -88,7 +90,7 @@ template <int D, int NW, int NC, int KC, int G, bool CAP, bool BIAS>
 __global__ __launch_bounds__((G * NW + NC) * kWave) __attribute__((amdgpu_waves_per_eu(2, NC ? 3 : 2))) void attn_varlen_mfma_kernel(Params pr) {
     constexpr int KS = D / 32, DT = D / 16, kBM = 32 * NW;
     constexpr bool kBySum = NW == 8;   // whether the probabilities' sum or the scores' maximum says when the reference moves (attn_mfma.hip)
-    constexpr bool kMod = CAP || BIAS;  // scores are in units of log2 e before the softmax, not raw
+    // (a cap leaves scores in units of log2 e, otherwise they are raw: what the product gives)
     using TileT = Tile<D, NC ? NC : NW, KC>;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem_raw[];
     const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lb = lane >> 4;
@@ -117,21 +119,29 @@ __global__ __launch_bounds__((G * NW + NC) * kWave) __attribute__((amdgpu_waves_
     const bf16_t *const k = pr.k + row0 * pr.mod.ldk, *const v = pr.v + row0 * pr.mod.ldv;
     const int32_t *const pos = BIAS && pr.mod.pos ? pr.mod.pos + row0 : nullptr;
     const int t0 = level * kBM;
-    const int tq0 = t0 + 32 * w + lr, tq1 = tq0 + 16;  // this lane's rows of the sequence (tiles 0 and 1)
     auto limit = [&](int t) { return min(max(t + 1, t < vis ? vis : 0), T); };  // keys that row t sees
-    const int lim[2] = {limit(tq0), limit(tq1)};
     // first row of the wave, in a scalar register so that tests on it are real branches (the wave
     // index comes from threadIdx, which the compiler cannot prove uniform)
     const int wq0 = __builtin_amdgcn_readfirstlane(t0 + 32 * w);
+    auto row = [&](int qt) { return wq0 + 16 * qt + lr; };  // this lane's rows of the sequence (tiles 0 and 1)
     const int wlo = limit(wq0), whi = wq0 < T ? limit(wq0 + 31) < wlo ? wlo : limit(wq0 + 31) : 0;  // keys that every / any row of the wave sees
     const int nkeys = max(min(T, t0 + kBM), t0 < vis ? vis : 0);
     const int nchunk = (nkeys + KC - 1) / KC, nstep = (nchunk + G - 1) / G;
+
+    // Chunks in the order they are taken.  With a bias the nearest keys come first, those of the workgroup's own rows and then back to the
+    // first, then the ones ahead (a prefix): from far to near the softmax reference would move in every block.  8320 tokens, 32 heads of 128,
+    // slopes up to 1: 846 us in the order of the keys.
+    const int own = min(t0 + kBM, nkeys) - 1, nearest = own / KC;
+    auto chunk_at = [&](int i) { return BIAS && i <= nearest ? nearest - i : i; };
 
     using AT = typename TileT::A;
     const int cw = NC ? wv - G * NW : w;
     const uint32_t k_row = (uint32_t)pr.mod.ldk * 2, v_row = (uint32_t)pr.mod.ldv * 2, kv_col = (uint32_t)kvh * D * 2;
     // requests a chunk into buffer b of a group's tiles; rows past T re-read row T - 1
     auto stage = [&](TileT &dst, int chunk, int b) __attribute__((always_inline)) {
+        const int at = cw * kWave + lane, key = min(chunk * KC + at, T - 1);
+        int32_t key_pos = key;  // (asked for before the copies, which it would else wait for)
+        if (BIAS && pos && at < KC) key_pos = pos[key];
 #pragma unroll
         for (int i = 0; i < AT::kIssues; ++i) {
             int row, cv;
@@ -147,12 +157,8 @@ __global__ __launch_bounds__((G * NW + NC) * kWave) __attribute__((amdgpu_waves_
             AT::issue(reinterpret_cast<const char *>(v) + off, &dst.v[b], cw, i);
         }
         if constexpr (BIAS) {
-            const int at = cw * kWave + lane;
             static_assert(KC <= (NC ? NC : NW) * kWave, "one position a lane");
-            if (at < KC) {
-                const int key = min(chunk * KC + at, T - 1);
-                dst.pos[b][at] = (float)(pos ? pos[key] : key);
-            }
+            if (at < KC) dst.pos[b][at] = (float)key_pos;
         }
     };
     // Chunks with keys that not every row of the workgroup sees: values that are not finite are taken out, by the wave that copied
@@ -168,10 +174,10 @@ __global__ __launch_bounds__((G * NW + NC) * kWave) __attribute__((amdgpu_waves_
         // (the chunk after a group's last one: clamped rows, never read)
         auto stage_step = [&](int step) __attribute__((always_inline)) {
 #pragma unroll
-            for (int gr = 0; gr < G; ++gr) stage(all[gr], step * G + gr, step & 1);
+            for (int gr = 0; gr < G; ++gr) stage(all[gr], chunk_at(step * G + gr), step & 1);
             async_tile_wait();
 #pragma unroll
-            for (int gr = 0; gr < G; ++gr) hide(all[gr], step * G + gr, step & 1);
+            for (int gr = 0; gr < G; ++gr) hide(all[gr], chunk_at(step * G + gr), step & 1);
             lds_barrier();
         };
         stage_step(0);
@@ -187,7 +193,7 @@ __global__ __launch_bounds__((G * NW + NC) * kWave) __attribute__((amdgpu_waves_
     bf16x8 bq[2][KS];
     {
         const bf16_t *const q = pr.q + row0 * pr.mod.ldq + (size_t)h * D + 8 * lb;
-        const bf16_t *qp0 = q + (size_t)min(tq0, T - 1) * pr.mod.ldq, *qp1 = q + (size_t)min(tq1, T - 1) * pr.mod.ldq;
+        const bf16_t *qp0 = q + (size_t)min(row(0), T - 1) * pr.mod.ldq, *qp1 = q + (size_t)min(row(1), T - 1) * pr.mod.ldq;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
             bq[0][ks] = *reinterpret_cast<const bf16x8 *>(qp0 + 32 * ks);
@@ -196,9 +202,10 @@ __global__ __launch_bounds__((G * NW + NC) * kWave) __attribute__((amdgpu_waves_
     }
     float pos_q[2] = {0.f, 0.f}, slope = 0.f;
     if constexpr (BIAS) {
-        slope = pr.mod.slopes[h] * kLog2e;
-        pos_q[0] = (float)(pos ? pos[min(tq0, T - 1)] : tq0);
-        pos_q[1] = (float)(pos ? pos[min(tq1, T - 1)] : tq1);
+        slope = CAP ? pr.mod.slopes[h] * kLog2e : pr.mod.slopes[h] / pr.mod.scale;  // in the scores' units
+        slope = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, slope)));  // (a scalar register)
+        pos_q[0] = (float)(pos ? pos[min(row(0), T - 1)] : row(0));
+        pos_q[1] = (float)(pos ? pos[min(row(1), T - 1)] : row(1));
     }
 
     // O^T tiles: oacc[dt][qt][r] = channel 16 dt + 4 lb + r of query (qt, lr)
@@ -207,20 +214,21 @@ __global__ __launch_bounds__((G * NW + NC) * kWave) __attribute__((amdgpu_waves_
     for (int dt = 0; dt < DT; ++dt) oacc[dt][0] = oacc[dt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
     // per query tile; l_run: this lane group's share of the row sum
     float m_run[2] = {-INFINITY, -INFINITY}, m_neg[2] = {0.f, 0.f}, l_run[2] = {0.f, 0.f};
-    const float scale2 = kMod ? 1.f : pr.scale2, lazy_raw = kLazy / scale2;  // scores' units -> log2
+    const float scale2 = CAP ? 1.f : pr.scale2, lazy_raw = kLazy / scale2;  // scores' units -> log2
 
     constexpr int kRowB = TileT::kPitch * 2;  // row pitch of the tiles in bytes
     if (NC == 0) {
-        stage(lds, grp, 0);
+        stage(lds, chunk_at(grp), 0);
         async_tile_wait();
-        hide(lds, grp, 0);
+        hide(lds, chunk_at(grp), 0);
     }
     lds_barrier();  // the groups' first chunks have landed
     for (int step = 0; step < nstep; ++step) {
-        const int cur = step & 1, chunk = step * G + grp;
-        if (NC == 0) stage(lds, chunk + G, cur ^ 1);  // the group's next chunk (past the last chunk: clamped rows, never read)
+        const int cur = step & 1, chunk = chunk_at(step * G + grp), next = chunk_at((step + 1) * G + grp);
+        if (NC == 0) stage(lds, next, cur ^ 1);  // the group's next chunk (past the last chunk: clamped rows, never read)
 #pragma unroll
-        for (int kt = 0; kt < KC / 32; ++kt) {
+        for (int kn = 0; kn < KC / 32; ++kn) {
+            const int kt = BIAS ? KC / 32 - 1 - kn : kn;  // (nearest first, as far as the chunks go back)
             const int kb = chunk * KC + 32 * kt;
             if (kb < whi) {  // uniform per wave
                 // all key fragments of the 32 keys first (one LDS round trip, not one per product):
@@ -240,45 +248,66 @@ __global__ __launch_bounds__((G * NW + NC) * kWave) __attribute__((amdgpu_waves_
                 // matrix instruction that waits behind its vector instructions leaves the matrix pipe idle
                 __builtin_amdgcn_s_setprio(2);
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks)
+                for (int ks = 0; ks < KS; ++ks) {
 #pragma unroll
                     for (int j = 0; j < 2; ++j)
 #pragma unroll
                         for (int qt = 0; qt < 2; ++qt) sacc[qt][j] = mfma16(kf[j][ks], bq[qt][ks], sacc[qt][j]);
+                }
                 __builtin_amdgcn_s_setprio(0);
                 // the transposed V fragments are requested now and arrive during the softmax: lane group lb
                 // passes rows 4 lb + lr / 4 (then + 16) and columns 4 (lr % 4) of a 16-channel tile and
                 // receives, for channel lr, the keys 4 lb .. 4 lb + 3 (then 16 + 4 lb ..): the slot order of P
-                // (64 channels now -- with a bias once it is added, its registers are needed until then; the other 64 are requested
-                // after the softmax, when the score registers are free)
+                // (64 channels now -- with a bias once it is in, its registers are needed until then; the other 64 are requested after the
+                // softmax, when the score registers are free)
                 strd_s16x4 vr8[DT / 4][8];
                 const bf16_t *vp = lds.v[cur].at(32 * kt + 4 * lb + (lr >> 2), 4 * (lr & 3));
                 if constexpr (!BIAS)
                     lds_issue_tr8<0, 16 * kRowB, 32, 16 * kRowB + 32, 64, 16 * kRowB + 64, 96, 16 * kRowB + 96>(vp, vr8[0]);
-                if constexpr (kMod) {
+                if constexpr (CAP) {
+                    float far = 0.f;
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        f32x4 pk;
-                        if constexpr (BIAS) pk = *reinterpret_cast<const f32x4 *>(&lds.pos[cur][32 * kt + 16 * j + 4 * lb]);
+                    for (int qt = 0; qt < 2; ++qt)
+#pragma unroll
+                        for (int j = 0; j < 2; ++j)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) far = fmaxf(far, fabsf(sacc[qt][j][r]));
+                    if (__builtin_expect(__any(far > pr.near), 0)) {
 #pragma unroll
                         for (int qt = 0; qt < 2; ++qt)
 #pragma unroll
-                            for (int r = 0; r < 4; ++r) {
-                                float x;
-                                if constexpr (CAP)
-                                    x = fmaf(-2.f * pr.c2, __builtin_amdgcn_rcpf(ex2(sacc[qt][j][r] * pr.kappa) + 1.f), pr.c2);
-                                else
-                                    x = sacc[qt][j][r] * pr.scale2;
-                                if constexpr (BIAS) x = fmaf(-slope, fabsf(pk[r] - pos_q[qt]), x);
-                                sacc[qt][j][r] = x;
-                            }
+                            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                                for (int r = 0; r < 4; ++r)
+                                    sacc[qt][j][r] = fmaf(pr.c2_twice, __builtin_amdgcn_rcpf(ex2(sacc[qt][j][r] * pr.kappa) + 1.f), pr.c2);
+                    } else {
+#pragma unroll
+                        for (int qt = 0; qt < 2; ++qt)
+#pragma unroll
+                            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                                for (int r = 0; r < 4; ++r) {
+                                    const float y = sacc[qt][j][r], w = y * y;
+                                    sacc[qt][j][r] = y * fmaf(w, fmaf(w, fmaf(w, pr.tanh[3], pr.tanh[2]), pr.tanh[1]), pr.tanh[0]);
+                                }
                     }
                 }
-                if constexpr (BIAS)
-                    lds_issue_tr8<0, 16 * kRowB, 32, 16 * kRowB + 32, 64, 16 * kRowB + 64, 96, 16 * kRowB + 96>(vp, vr8[0]);
+                if constexpr (BIAS) {
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const f32x4 pk = *reinterpret_cast<const f32x4 *>(&lds.pos[cur][32 * kt + 16 * j + 4 * lb]);
+#pragma unroll
+                        for (int qt = 0; qt < 2; ++qt)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) sacc[qt][j][r] = fmaf(-slope, fabsf(pk[r] - pos_q[qt]), sacc[qt][j][r]);
+                    }
+                }
                 const bool edge = kb + 32 > wlo;  // uniform: some (key, query) pair of the block is masked
                 if (edge) {
-                    asm volatile("" ::);  // keeps this a branch: folded into selects it would run for every block
+                    // (hides the row: keeps this a branch -- folded into selects it would run for every block -- and the limits out of registers)
+                    int first = row(0);
+                    asm volatile("" : "+v"(first));
+                    const int lim[2] = {limit(first), limit(first + 16)};
 #pragma unroll
                     for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -288,6 +317,8 @@ __global__ __launch_bounds__((G * NW + NC) * kWave) __attribute__((amdgpu_waves_
                             if (key >= lim[1]) sacc[1][j][r] = -INFINITY;
                         }
                 }
+                if constexpr (BIAS)
+                    lds_issue_tr8<0, 16 * kRowB, 32, 16 * kRowB + 32, 64, 16 * kRowB + 64, 96, 16 * kRowB + 96>(vp, vr8[0]);
                 // The probabilities, against the reference as it is (of a row that has seen no key yet: 0).  The row sum is taken of
                 // them as they enter the second product, i.e. rounded to bf16 (numerator and denominator then carry the same
                 // rounding), two at a time.
@@ -300,7 +331,7 @@ __global__ __launch_bounds__((G * NW + NC) * kWave) __attribute__((amdgpu_waves_
                         for (int j = 0; j < 2; ++j)
 #pragma unroll
                             for (int r = 0; r < 4; ++r)
-                                pf[qt][4 * j + r] = (bf16_t)ex2(kMod ? sacc[qt][j][r] + m_neg[qt] : fmaf(sacc[qt][j][r], scale2, m_neg[qt]));
+                                pf[qt][4 * j + r] = (bf16_t)ex2(CAP ? sacc[qt][j][r] + m_neg[qt] : fmaf(sacc[qt][j][r], scale2, m_neg[qt]));
                         ps[qt] = kBySum ? 0.f : l_run[qt];
 #pragma unroll
                         for (int e = 0; e < 8; e += 2)
@@ -377,7 +408,7 @@ __global__ __launch_bounds__((G * NW + NC) * kWave) __attribute__((amdgpu_waves_
         }
         if (NC == 0) {
             async_tile_wait();
-            hide(lds, chunk + G, cur ^ 1);
+            hide(lds, next, cur ^ 1);
         }
         lds_barrier();  // the next chunk has landed, every wave is done with this one
     }
@@ -422,6 +453,7 @@ __global__ __launch_bounds__((G * NW + NC) * kWave) __attribute__((amdgpu_waves_
     if (__builtin_expect(odd, 0)) {
         // The values left out of the products, for the rows that see them.  A probability is above 0 and a finite factor leaves such a
         // value as it is, so the value itself is added.
+        const int lim[2] = {limit(row(0)), limit(row(1))};
 #pragma unroll 1
         for (int key = wg_lo / KC * KC; key < whi; ++key) {
 #pragma unroll
@@ -438,7 +470,7 @@ __global__ __launch_bounds__((G * NW + NC) * kWave) __attribute__((amdgpu_waves_
     }
 #pragma unroll
     for (int qt = 0; qt < 2; ++qt) {
-        const int tq = qt ? tq1 : tq0;
+        const int tq = row(qt);
         if (tq < T) {
             const float inv = 1.f / l_run[qt];
             bf16_t *op = pr.o + ((row0 + tq) * pr.Hq + h) * D + 4 * lb;
@@ -475,7 +507,12 @@ int launch(Params &pr, const strd_seq *seqs, int nseq, hipStream_t st) {
 template <int D>
 int launch_d(Params &pr, const strd_seq *seqs, int nseq, long long blocks128, long long blocks256, int longest, hipStream_t st) {
     const int Hq = pr.Hq;
-    const bool big = blocks256 * Hq >= 384;
+    // In causal order as for one sequence (attn_mfma.hip).  With a prefix the blocks of a sequence cost the same, and what counts is the
+    // rounds of the chip: one of 256 rows a workgroup takes 1.6 times one of 128, with heads of 64 a little over 1.4 (2176 tokens, 32 heads of 128, 2
+    // rounds / 3: 106 / 103 us; 28 heads of 64, 1 / 2: 49 / 55; six sequences of 2534 tokens, 32 heads of 64, 2 / 3: 39 / 49).
+    const long long rounds256 = (blocks256 * Hq + 255) / 256, rounds128 = (blocks128 * Hq + 255) / 256;
+    const bool fewer = D == 128 ? 8 * rounds256 < 5 * rounds128 : 10 * rounds256 <= 7 * rounds128;
+    const bool big = pr.mod.prefix ? longest > 256 && fewer : blocks256 * Hq >= 384;
     const bool one = longest <= 256 || blocks128 * Hq > 512 + (D == 128 ? 7 : 4) * blocks128;
     return big   ? launch<D, 8, 4, 128, 1>(pr, seqs, nseq, st)
            : one ? launch<D, 4, 0, 64, 1>(pr, seqs, nseq, st)
@@ -500,7 +537,14 @@ int attn_varlen_mfma(const void *q, const void *k, const void *v, void *o, int H
     pr.Hq = Hq, pr.Hkv = Hkv;
     pr.scale2 = mod.scale * kLog2e;
     pr.kappa = 2.f * kLog2e * mod.scale * mod.inv_cap;
-    pr.c2 = mod.cap * kLog2e;
+    pr.c2 = mod.cap * kLog2e, pr.c2_twice = -2.f * pr.c2;
+    // tanh(y) / y up to y = 0.5, of least relative error (5.5e-7); y = ky raw goes into the coefficients.  Where those of the higher powers
+    // leave fp32's range (a cap far above every score) the polynomial ends before they count, where they are too large (a cap far below) the
+    // exponential form, whose absolute error is a few steps of the cap, takes every score.
+    const double tanh_y[4] = {0.999999452, -0.333263082, 0.131902465, -0.0444017053}, ky = (double)mod.scale * mod.inv_cap;
+    pr.near = ky > 1e4 ? -1.f : fminf((float)((ky > 1e-5 ? 0.5 : ky > 1e-9 ? 0.05 : 1e-3) / ky), 1e18f);
+    double power = (double)mod.scale * kLog2e;
+    for (int i = 0; i < 4; ++i, power *= ky * ky) pr.tanh[i] = (float)(tanh_y[i] * power);
     pr.mod = mod;
     // XCD-aware order when the kv heads per XCD and the query heads per kv head are powers of two
     const int per = Hkv / kXcd, gq = Hq / Hkv;

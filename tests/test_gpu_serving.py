@@ -93,6 +93,31 @@ def test_prefill_varlen_spread_scores(dtype, d):
     _within(o, want, _out_bound(want, es, mag, dtype, 430), "o")
 
 
+@pytest.mark.parametrize("dtype,d", [(F32, 64), (BF16, 64), (BF16, 128), (BF16, 96)])
+@pytest.mark.parametrize("cap", [1e5, 1e7, 1e10, 3e38])
+def test_prefill_varlen_caps_far_above_the_scores(cap, dtype, d):
+    """Such a cap leaves scores of up to 30 as they are: 30^3 / (3 cap^2) is below a step.  Its form may add ten roundings of a score, which a
+    second share of the score's own bound ((d + 2) roundings of the sum of |q| |k|) covers."""
+    _say("far cap", cap, dtype, d)
+    seqs = [(200, 30, 0), (90, 0, 0)]
+    q, k, v, _, _ = _prefill(seqs, 4, 2, d, dtype, 0.0, False, False, True, seed=4, size=4.0)
+    o = strd.attn_prefill_varlen(_dev(q), _dev(k), _dev(v), seqs, prefix=True, cap=cap)
+    want, es, mag = plain.attn_varlen(np64(q), np64(k), np64(v), seqs, True, 0.0, None, None)
+    _within(o, want, _out_bound(want, 2 * es, mag, dtype, 230), "o")
+
+
+@pytest.mark.parametrize("cap", [1e-38, 1e-3])
+@pytest.mark.parametrize("dtype,d", [(F32, 64), (BF16, 128)])
+def test_prefill_varlen_caps_far_below_the_scores(cap, dtype, d):
+    """What is left of the scores is within cap of 0: every key a row sees counts the same to within 2 cap (and its roundings)."""
+    _say("near cap", cap, dtype, d)
+    seqs = [(100, 30, 0)]
+    q, k, v, _, _ = _prefill(seqs, 4, 2, d, dtype, 0.0, False, False, False, seed=4)
+    o = strd.attn_prefill_varlen(_dev(q), _dev(k), _dev(v), seqs, cap=cap)
+    want, es, mag = plain.attn_varlen(np64(q), np64(k), np64(v), seqs, False, cap, None, None)
+    _within(o, want, _out_bound(want, es, mag, dtype, 130), "o")
+
+
 @pytest.mark.parametrize("dtype,d,Hkv", [(F32, 64, 2), (BF16, 128, 2), (BF16, 64, 4), (BF16, 72, 1)])
 def test_prefill_varlen_takes_column_ranges_of_a_projection(dtype, d, Hkv):
     _say("pitched", dtype, d, Hkv)
@@ -312,6 +337,18 @@ def test_decode_spread_scores(d, dtype, kv4):
     k *= torch.linspace(0.1, 2.0, 1500)[:, None, None].to(dtype)
     k[1203] = (3 * q.view(2, 4, d)[:, 1]).to(dtype)
     _decode_check(q, k, v, sl, ps, w, 0.0, kv4)
+
+
+@pytest.mark.parametrize("cap", [1e-38, 1e7, 3e38])
+@pytest.mark.parametrize("d,dtype", [(64, BF16), (128, BF16), (96, BF16), (128, F32)])
+def test_decode_caps_far_from_the_scores(cap, d, dtype):
+    """Far above them it leaves them as they are (see the packed form's test), far below it leaves nothing of them."""
+    _say("decode far cap", cap, d, dtype)
+    q, k, v, _, _, w = _decode_case(333, 8, 2, d, dtype, False, False, False, size=4.0)
+    o, got = strd.attn_decode_step_weights(_dev(q), _dev(k), _dev(v), cap=cap, weights=_dev(w))
+    want, ww, es, mag, ew = plain.decode(np64(q), np64(k), np64(v), cap if cap < 1 else 0.0, None, None, np64(w))
+    _within(o, want, _out_bound(want, 2 * es, mag, dtype, 333), "o")
+    _within(got, ww, 2 * ew + 333 * plain.U32 * np.abs(ww) + 1e-30, "weights")
 
 
 @pytest.mark.parametrize("kv4", [True, False])
