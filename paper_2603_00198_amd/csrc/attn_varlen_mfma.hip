@@ -87,7 +87,7 @@ struct Params {
 // G groups of NW computing waves, and NC copy waves that serve all groups; NC = 0: the computing waves request the copies of
 // their group themselves.  Group g takes chunks g, g + G, ...
 template <int D, int NW, int NC, int KC, int G, bool CAP, bool BIAS>
-__global__ __launch_bounds__((G * NW + NC) * kWave) __attribute__((amdgpu_waves_per_eu(2, NC ? 3 : 2))) void attn_varlen_mfma_kernel(Params pr) {
+__global__ __launch_bounds__((G * NW + NC) * kWave) __attribute__((amdgpu_waves_per_eu(2, NC ? 3 : D == 64 ? 4 : 2))) void attn_varlen_mfma_kernel(Params pr) {
     constexpr int KS = D / 32, DT = D / 16, kBM = 32 * NW;
     constexpr bool kBySum = NW == 8;   // whether the probabilities' sum or the scores' maximum says when the reference moves (attn_mfma.hip)
     // (a cap leaves scores in units of log2 e, otherwise they are raw: what the product gives)
@@ -137,24 +137,40 @@ __global__ __launch_bounds__((G * NW + NC) * kWave) __attribute__((amdgpu_waves_
     using AT = typename TileT::A;
     const int cw = NC ? wv - G * NW : w;
     const uint32_t k_row = (uint32_t)pr.mod.ldk * 2, v_row = (uint32_t)pr.mod.ldv * 2, kv_col = (uint32_t)kvh * D * 2;
+    // Where this lane's copies of a chunk start, from its first row, which copy waves hold: a whole chunk takes no more than its base (keys
+    // and values of one pitch).  Waves that compute as well have no registers for it.
+    struct From {
+        uint32_t at[AT::kIssues];
+    };
+    auto starts = [&](From &from) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < AT::kIssues; ++i) {
+            int row, cv;
+            AT::slot(cw, lane, i, row, cv);
+            from.at[i] = (uint32_t)row * k_row + kv_col + (uint32_t)cv * 16;
+        }
+    };
     // requests a chunk into buffer b of a group's tiles; rows past T re-read row T - 1
-    auto stage = [&](TileT &dst, int chunk, int b) __attribute__((always_inline)) {
+    auto stage = [&](TileT &dst, int chunk, int b, const From &from) __attribute__((always_inline)) {
         const int at = cw * kWave + lane, key = min(chunk * KC + at, T - 1);
         int32_t key_pos = key;  // (asked for before the copies, which it would else wait for)
         if (BIAS && pos && at < KC) key_pos = pos[key];
+        if (NC > 0 && (chunk + 1) * KC <= T && k_row == v_row) {  // uniform
+            const char *const kc = reinterpret_cast<const char *>(k) + (size_t)chunk * KC * k_row;
+            const char *const vc = reinterpret_cast<const char *>(v) + (size_t)chunk * KC * v_row;
 #pragma unroll
-        for (int i = 0; i < AT::kIssues; ++i) {
-            int row, cv;
-            AT::slot(cw, lane, i, row, cv);
-            const uint32_t off = (uint32_t)min(chunk * KC + row, T - 1) * k_row + kv_col + (uint32_t)cv * 16;
-            AT::issue(reinterpret_cast<const char *>(k) + off, &dst.k[b], cw, i);
-        }
+            for (int i = 0; i < AT::kIssues; ++i) AT::issue(kc + from.at[i], &dst.k[b], cw, i);
 #pragma unroll
-        for (int i = 0; i < AT::kIssues; ++i) {
-            int row, cv;
-            AT::slot(cw, lane, i, row, cv);
-            const uint32_t off = (uint32_t)min(chunk * KC + row, T - 1) * v_row + kv_col + (uint32_t)cv * 16;
-            AT::issue(reinterpret_cast<const char *>(v) + off, &dst.v[b], cw, i);
+            for (int i = 0; i < AT::kIssues; ++i) AT::issue(vc + from.at[i], &dst.v[b], cw, i);
+        } else {
+#pragma unroll
+            for (int i = 0; i < AT::kIssues; ++i) {
+                int row, cv;
+                AT::slot(cw, lane, i, row, cv);
+                const uint32_t at_row = (uint32_t)min(chunk * KC + row, T - 1), col = kv_col + (uint32_t)cv * 16;
+                AT::issue(reinterpret_cast<const char *>(k) + (at_row * k_row + col), &dst.k[b], cw, i);
+                AT::issue(reinterpret_cast<const char *>(v) + (at_row * v_row + col), &dst.v[b], cw, i);
+            }
         }
         if constexpr (BIAS) {
             static_assert(KC <= (NC ? NC : NW) * kWave, "one position a lane");
@@ -171,10 +187,12 @@ __global__ __launch_bounds__((G * NW + NC) * kWave) __attribute__((amdgpu_waves_
     };
     static_assert(G == 1 || NC > 0, "a flag per wave that fills tiles");
     if (copies) {
+        From from;
+        starts(from);
         // (the chunk after a group's last one: clamped rows, never read)
         auto stage_step = [&](int step) __attribute__((always_inline)) {
 #pragma unroll
-            for (int gr = 0; gr < G; ++gr) stage(all[gr], chunk_at(step * G + gr), step & 1);
+            for (int gr = 0; gr < G; ++gr) stage(all[gr], chunk_at(step * G + gr), step & 1, from);
             async_tile_wait();
 #pragma unroll
             for (int gr = 0; gr < G; ++gr) hide(all[gr], chunk_at(step * G + gr), step & 1);
@@ -217,15 +235,16 @@ __global__ __launch_bounds__((G * NW + NC) * kWave) __attribute__((amdgpu_waves_
     const float scale2 = CAP ? 1.f : pr.scale2, lazy_raw = kLazy / scale2;  // scores' units -> log2
 
     constexpr int kRowB = TileT::kPitch * 2;  // row pitch of the tiles in bytes
+    From from;
     if (NC == 0) {
-        stage(lds, chunk_at(grp), 0);
+        stage(lds, chunk_at(grp), 0, from);
         async_tile_wait();
         hide(lds, chunk_at(grp), 0);
     }
     lds_barrier();  // the groups' first chunks have landed
     for (int step = 0; step < nstep; ++step) {
         const int cur = step & 1, chunk = chunk_at(step * G + grp), next = chunk_at((step + 1) * G + grp);
-        if (NC == 0) stage(lds, next, cur ^ 1);  // the group's next chunk (past the last chunk: clamped rows, never read)
+        if (NC == 0) stage(lds, next, cur ^ 1, from);  // the group's next chunk (past the last chunk: clamped rows, never read)
 #pragma unroll
         for (int kn = 0; kn < KC / 32; ++kn) {
             const int kt = BIAS ? KC / 32 - 1 - kn : kn;  // (nearest first, as far as the chunks go back)
@@ -507,16 +526,23 @@ int launch(Params &pr, const strd_seq *seqs, int nseq, hipStream_t st) {
 template <int D>
 int launch_d(Params &pr, const strd_seq *seqs, int nseq, long long blocks128, long long blocks256, int longest, hipStream_t st) {
     const int Hq = pr.Hq;
-    // In causal order as for one sequence (attn_mfma.hip).  With a prefix the blocks of a sequence cost the same, and what counts is the
-    // rounds of the chip: one of 256 rows a workgroup takes 1.6 times one of 128, with heads of 64 a little over 1.4 (2176 tokens, 32 heads of 128, 2
-    // rounds / 3: 106 / 103 us; 28 heads of 64, 1 / 2: 49 / 55; six sequences of 2534 tokens, 32 heads of 64, 2 / 3: 39 / 49).
-    const long long rounds256 = (blocks256 * Hq + 255) / 256, rounds128 = (blocks128 * Hq + 255) / 256;
-    const bool fewer = D == 128 ? 8 * rounds256 < 5 * rounds128 : 10 * rounds256 <= 7 * rounds128;
-    const bool big = pr.mod.prefix ? longest > 256 && fewer : blocks256 * Hq >= 384;
-    const bool one = longest <= 256 || blocks128 * Hq > 512 + (D == 128 ? 7 : 4) * blocks128;
-    return big   ? launch<D, 8, 4, 128, 1>(pr, seqs, nseq, st)
-           : one ? launch<D, 4, 0, 64, 1>(pr, seqs, nseq, st)
-                 : launch<D, 4, 4, 64, 2>(pr, seqs, nseq, st);
+    const long long wgs128 = blocks128 * Hq, wgs256 = blocks256 * Hq;
+    if constexpr (D == 64) {
+        // Four workgroups of four waves fit a CU, and pass one of 256 rows (8320 tokens, 28 heads: 279 / 286 us, with a cap and a bias 410 / 441;
+        // six sequences of 3493 tokens and a prefix 43 / 50).  Few of them: two groups of waves with a copying one, each on half of the keys (2981
+        // tokens, 28 heads 57 / 53 us; 2176 tokens, 32 heads 44 / 40, with a prefix 62 / 66; 3493 tokens in six, 28 heads 31 / 41).
+        const bool one = longest <= 256 || wgs128 > (pr.mod.prefix ? 512 : 640 + 4 * blocks128);
+        return one ? launch<D, 4, 0, 64, 1>(pr, seqs, nseq, st) : launch<D, 4, 4, 64, 2>(pr, seqs, nseq, st);
+    } else {
+        // In causal order as for one sequence (attn_mfma.hip).  With a prefix the blocks of a sequence cost the same, and what counts is the
+        // rounds of the chip: one of 256 rows a workgroup takes 1.6 times one of 128 (2176 tokens, 32 heads, 2 rounds / 3: 106 / 103 us).
+        const long long rounds256 = (wgs256 + 255) / 256, rounds128 = (wgs128 + 255) / 256;
+        const bool big = pr.mod.prefix ? longest > 256 && 8 * rounds256 < 5 * rounds128 : wgs256 >= 384;
+        const bool one = longest <= 256 || wgs128 > 512 + 7 * blocks128;
+        return big   ? launch<D, 8, 4, 128, 1>(pr, seqs, nseq, st)
+               : one ? launch<D, 4, 0, 64, 1>(pr, seqs, nseq, st)
+                     : launch<D, 4, 4, 64, 2>(pr, seqs, nseq, st);
+    }
 }
 
 }  // namespace
