@@ -4,9 +4,9 @@
 //  * Blocks are dealt by level over the sequences (AttnTab), the longest first; rows have pitches.
 //  * A row sees the keys before its limit: its own number + 1, or its sequence's vision rows.  Limits never fall from one row to
 //    the next, so a wave meets at most two 32-key blocks that only some of its rows see.
-//  * A score becomes cap * tanh(score / cap): where the scores of a block are up to cap / 2, a polynomial in the square (five
-//    instructions), else c - 2 c / (2^(score * 2 log2 e / cap) + 1) in units of log2 e, with two transcendental instructions of a quarter's
-//    rate beside the softmax's one.  The bias takes the rows' positions from LDS, where they lie as fp32 numbers beside the keys.
+//  * A score becomes cap * tanh(score / cap): where the scores of a block are up to cap / 4, a polynomial in the square that takes
+//    three more instructions than a score without, up to cap / 2 four, else c - 2 c / (2^(score * 2 log2 e / cap) + 1) in units of log2 e, with two
+//    transcendental instructions of a quarter's rate beside the softmax's one.  The bias takes the rows' positions from LDS, where they lie as fp32 numbers beside the keys.
 //  * What a row does not see does not reach it.  A probability of 0 takes a value out of the second product only if it is finite: in
 //    chunks with hidden keys the values are looked at when they have landed in LDS, and those that are not finite are taken out and
 //    added at the end, row by row.  And a row's softmax reference moves by the row's own scores alone, never because of a neighbour in its wave: a row's
@@ -79,8 +79,9 @@ struct Params {
     bf16_t *o;
     int Hq, Hkv, xcd_map;
     float scale2;              // scale * log2 e
-    float near, kappa, c2, c2_twice;  // with a cap: raw scores up to which the polynomial holds, 2 log2 e * scale / cap, cap * log2 e, -2 cap * log2 e
-    float tanh[4];             // cap log2 e tanh(raw scale / cap) / raw in powers of raw^2
+    // with a cap: raw scores that are a quarter and half of it, 2 log2 e * scale / cap, cap * log2 e, -2 cap * log2 e
+    float near, half, kappa, c2, c2_twice;
+    float tanh_near[3], tanh_half[4];  // cap log2 e tanh(raw scale / cap) / raw in powers of raw^2, up to those
     AttnMod mod;
 };
 
@@ -284,6 +285,7 @@ __global__ __launch_bounds__((G * NW + NC) * kWave) __attribute__((amdgpu_waves_
                 if constexpr (!BIAS)
                     lds_issue_tr8<0, 16 * kRowB, 32, 16 * kRowB + 32, 64, 16 * kRowB + 64, 96, 16 * kRowB + 96>(vp, vr8[0]);
                 if constexpr (CAP) {
+                    // (less the row's reference, added in the same instruction: the exponents as they are, unless the reference moves)
                     float far = 0.f;
 #pragma unroll
                     for (int qt = 0; qt < 2; ++qt)
@@ -292,13 +294,27 @@ __global__ __launch_bounds__((G * NW + NC) * kWave) __attribute__((amdgpu_waves_
 #pragma unroll
                             for (int r = 0; r < 4; ++r) far = fmaxf(far, fabsf(sacc[qt][j][r]));
                     if (__builtin_expect(__any(far > pr.near), 0)) {
+                        if (__any(far > pr.half)) {
 #pragma unroll
-                        for (int qt = 0; qt < 2; ++qt)
+                            for (int qt = 0; qt < 2; ++qt) {
+                                const float top = pr.c2 + m_neg[qt];
 #pragma unroll
-                            for (int j = 0; j < 2; ++j)
+                                for (int j = 0; j < 2; ++j)
 #pragma unroll
-                                for (int r = 0; r < 4; ++r)
-                                    sacc[qt][j][r] = fmaf(pr.c2_twice, __builtin_amdgcn_rcpf(ex2(sacc[qt][j][r] * pr.kappa) + 1.f), pr.c2);
+                                    for (int r = 0; r < 4; ++r)
+                                        sacc[qt][j][r] = fmaf(pr.c2_twice, __builtin_amdgcn_rcpf(ex2(sacc[qt][j][r] * pr.kappa) + 1.f), top);
+                            }
+                        } else {
+#pragma unroll
+                            for (int qt = 0; qt < 2; ++qt)
+#pragma unroll
+                                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                                    for (int r = 0; r < 4; ++r) {
+                                        const float y = sacc[qt][j][r], w = y * y;
+                                        sacc[qt][j][r] = fmaf(y, fmaf(w, fmaf(w, fmaf(w, pr.tanh_half[3], pr.tanh_half[2]), pr.tanh_half[1]), pr.tanh_half[0]), m_neg[qt]);
+                                    }
+                        }
                     } else {
 #pragma unroll
                         for (int qt = 0; qt < 2; ++qt)
@@ -307,7 +323,7 @@ __global__ __launch_bounds__((G * NW + NC) * kWave) __attribute__((amdgpu_waves_
 #pragma unroll
                                 for (int r = 0; r < 4; ++r) {
                                     const float y = sacc[qt][j][r], w = y * y;
-                                    sacc[qt][j][r] = y * fmaf(w, fmaf(w, fmaf(w, pr.tanh[3], pr.tanh[2]), pr.tanh[1]), pr.tanh[0]);
+                                    sacc[qt][j][r] = fmaf(y, fmaf(w, fmaf(w, pr.tanh_near[2], pr.tanh_near[1]), pr.tanh_near[0]), m_neg[qt]);
                                 }
                     }
                 }
@@ -350,7 +366,7 @@ __global__ __launch_bounds__((G * NW + NC) * kWave) __attribute__((amdgpu_waves_
                         for (int j = 0; j < 2; ++j)
 #pragma unroll
                             for (int r = 0; r < 4; ++r)
-                                pf[qt][4 * j + r] = (bf16_t)ex2(CAP ? sacc[qt][j][r] + m_neg[qt] : fmaf(sacc[qt][j][r], scale2, m_neg[qt]));
+                                pf[qt][4 * j + r] = (bf16_t)ex2(CAP ? sacc[qt][j][r] : fmaf(sacc[qt][j][r], scale2, m_neg[qt]));
                         ps[qt] = kBySum ? 0.f : l_run[qt];
 #pragma unroll
                         for (int e = 0; e < 8; e += 2)
@@ -371,6 +387,7 @@ __global__ __launch_bounds__((G * NW + NC) * kWave) __attribute__((amdgpu_waves_
                 // m_run is the reference the exponentials are taken against, common to the four lane groups of a query.  It
                 // follows the running max lazily (attn_mfma.hip): it moves when some lane of the QUERY sees a score more than 2^kLazy above
                 // it, or (kBySum) eight probabilities that add up to more than kLazySum, or the first key.
+                auto limit_of = [&](int qt) { return (CAP ? m_run[qt] + m_neg[qt] : m_run[qt]) + lazy_raw; };  // (of a maximum, -inf before the first key)
                 bool moves;
                 if constexpr (kBySum) {
                     probabilities();
@@ -378,7 +395,7 @@ __global__ __launch_bounds__((G * NW + NC) * kWave) __attribute__((amdgpu_waves_
                     if (moves) maxima();
                 } else {
                     maxima();
-                    moves = __any(tm[0] > m_run[0] + lazy_raw || tm[1] > m_run[1] + lazy_raw);
+                    moves = __any(tm[0] > limit_of(0) || tm[1] > limit_of(1));
                 }
                 if (moves) {
 #pragma unroll
@@ -388,16 +405,23 @@ __global__ __launch_bounds__((G * NW + NC) * kWave) __attribute__((amdgpu_waves_
                         t = fmaxf(t, __shfl_xor(t, 32, kWave));
                         why = fmaxf(why, __shfl_xor(why, 16, kWave));
                         why = fmaxf(why, __shfl_xor(why, 32, kWave));
-                        const bool own = m_run[qt] == -INFINITY || (kBySum ? why > kLazySum : why > m_run[qt] + lazy_raw);
+                        const bool own = m_run[qt] == -INFINITY || (kBySum ? why > kLazySum : why > limit_of(qt));
                         // (a row may not see any key of the groups behind the first, whose chunks start later)
-                        const float nm = own ? fmaxf(m_run[qt], t) : m_run[qt];
+                        const float nm = own ? fmaxf(m_run[qt], CAP ? t - m_neg[qt] : t) : m_run[qt];
                         const bool none = nm == -INFINITY;
                         const float corr = none ? 1.f : ex2((m_run[qt] - nm) * scale2);
                         l_run[qt] *= corr;
 #pragma unroll
                         for (int dt = 0; dt < DT; ++dt) oacc[dt][qt] *= corr;
                         m_run[qt] = nm;
-                        m_neg[qt] = none ? 0.f : -nm * scale2;
+                        const float neg = none ? 0.f : -nm * scale2;
+                        if constexpr (CAP) {
+#pragma unroll
+                            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                                for (int r = 0; r < 4; ++r) sacc[qt][j][r] += neg - m_neg[qt];
+                        }
+                        m_neg[qt] = neg;
                     }
                     if constexpr (kBySum) probabilities();
                 }
@@ -564,13 +588,18 @@ int attn_varlen_mfma(const void *q, const void *k, const void *v, void *o, int H
     pr.scale2 = mod.scale * kLog2e;
     pr.kappa = 2.f * kLog2e * mod.scale * mod.inv_cap;
     pr.c2 = mod.cap * kLog2e, pr.c2_twice = -2.f * pr.c2;
-    // tanh(y) / y up to y = 0.5, of least relative error (5.5e-7); y = ky raw goes into the coefficients.  Where those of the higher powers
-    // leave fp32's range (a cap far above every score) the polynomial ends before they count, where they are too large (a cap far below) the
-    // exponential form, whose absolute error is a few steps of the cap, takes every score.
-    const double tanh_y[4] = {0.999999452, -0.333263082, 0.131902465, -0.0444017053}, ky = (double)mod.scale * mod.inv_cap;
-    pr.near = ky > 1e4 ? -1.f : fminf((float)((ky > 1e-5 ? 0.5 : ky > 1e-9 ? 0.05 : 1e-3) / ky), 1e18f);
+    // tanh(y) / y up to y = 0.25 and 0.5, of least relative error (4.0e-7, 5.5e-7); y = ky raw goes into the coefficients.  Where those of the
+    // higher powers leave fp32's range (a cap far above every score) the polynomials end before they count, where they are too large (a cap far
+    // below) the exponential form, whose absolute error is a few steps of the cap, takes every score.
+    const double near_y[3] = {0.99999960434, -0.33321908205, 0.12841613181}, half_y[4] = {0.999999452, -0.333263082, 0.131902465, -0.0444017053};
+    const double ky = (double)mod.scale * mod.inv_cap;
+    pr.half = ky > 1e4 ? -1.f : fminf((float)((ky > 1e-5 ? 0.5 : ky > 1e-9 ? 0.05 : 1e-3) / ky), 1e18f);
+    pr.near = 0.5f * pr.half;
     double power = (double)mod.scale * kLog2e;
-    for (int i = 0; i < 4; ++i, power *= ky * ky) pr.tanh[i] = (float)(tanh_y[i] * power);
+    for (int i = 0; i < 4; ++i, power *= ky * ky) {
+        pr.tanh_half[i] = (float)(half_y[i] * power);
+        if (i < 3) pr.tanh_near[i] = (float)(near_y[i] * power);
+    }
     pr.mod = mod;
     // XCD-aware order when the kv heads per XCD and the query heads per kv head are powers of two
     const int per = Hkv / kXcd, gq = Hq / Hkv;
