@@ -13,12 +13,6 @@ struct ScoreMod {
     const float *slopes;            // [Hq] or null
     const int32_t *pos;             // [T] or null: the row number
 };
-// In units of log2 e.  tanhf and not an exponential form: the scores' errors are the weights' relative errors.
-__device__ __forceinline__ float capped_score(const ScoreMod &m, float dot) {
-    const float x = dot * m.scale;
-    return m.cap > 0.f ? m.cap * tanhf(x * m.inv_cap) : x;
-}
-
 struct CacheView {
     const void *k, *km, *v, *vm;  // plain: k and v; 4-bit: codes and (s, z) pairs
 };

@@ -106,7 +106,7 @@ __global__ __launch_bounds__(kThreads) void decode_cache_kernel(const T *__restr
 #pragma unroll
                         for (int e = 0; e < 8; ++e) dot = fmaf(qv[r][n][e], kx[u][n][e], dot);
                 const int t = t0 + kGroups * u;
-                x[u][r] = (capped_score(mod, group_sum(dot)) - slope[r] * far[u]) * kLog2e;
+                x[u][r] = (capped_score(group_sum(dot), mod.scale, mod.cap, mod.inv_cap) - slope[r] * far[u]) * kLog2e;
                 if (ws.scores && sub == 0 && r < nh && t < t_end) ws.scores[(size_t)(h0 + r) * ws.ldt + t] = x[u][r];
                 if (t < t_end) mn = fmaxf(mn, x[u][r]);
             }

@@ -200,6 +200,21 @@ __device__ __forceinline__ strd_bf16x8 tr_pair(strd_s16x4 lo, strd_s16x4 hi) {
 // waited for explicitly, by count, where their data is needed.
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
+// scale * dot, capped (strd.h; cap == 0: none).  Up to half of the cap tanh(y) / y is a polynomial in y^2 of least relative error
+// (1.3e-8); where some lane's score is beyond, tanhf and not an exponential form: the scores' errors are the weights' relative errors.
+__device__ __forceinline__ float capped_score(float dot, float scale, float cap, float inv_cap) {
+    const float x = dot * scale;
+    if (!(cap > 0.f)) return x;  // uniform
+    const float y = x * inv_cap, w = y * y;
+    float r = fmaf(w, 0.0171347708f, -0.0529858599f);
+    r = fmaf(w, r, 0.133247737f);
+    r = fmaf(w, r, -0.333330689f);
+    r = fmaf(w, r, 0.999999987f);
+    float t = y * r;
+    if (__any(!(fabsf(y) <= 0.5f))) t = fabsf(y) <= 0.5f ? t : tanhf(y);
+    return cap * t;
+}
+
 // Inclusive prefix sum of a float over the 64 lanes of a wave with DPP moves (no LDS round trip).
 __device__ __forceinline__ float wave_inclusive_scan_f32(float v) {
 #define STRD_DPP_FADD(ctrl, row_mask) \

@@ -871,6 +871,16 @@ __global__ __launch_bounds__(NW *kWave) __attribute__((amdgpu_waves_per_eu(DJ ==
     auto body = [&](auto edge, int trip) __attribute__((always_inline)) {
         const int key0 = trip * KT * 16, last = Tn - 1 - key0;  // uniform
         const T *kb = k + (size_t)key0 * ldk + (size_t)hk * d, *vb = v + (size_t)key0 * ldv + (size_t)hk * d;
+        int32_t pos_k[KT][4];  // (asked for first: loads return in order)
+        if constexpr (kMod) {
+#pragma unroll
+            for (int u = 0; u < KT; ++u)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int key = key0 + 16 * u + 4 * lb + i;
+                    pos_k[u][i] = pos ? pos[min(key, Tn - 1)] : key;
+                }
+        }
         Operand<T, KJ, FULL> kf[KT];
         float vf[KT][4][DJ][4];
 #pragma unroll
@@ -904,9 +914,8 @@ __global__ __launch_bounds__(NW *kWave) __attribute__((amdgpu_waves_per_eu(DJ ==
             for (int i = 0; i < 4; ++i) {
                 const int key = key0 + 16 * u + 4 * lb + i;
                 if constexpr (kMod) {  // in units of log2 e from here on (scale2 is 1)
-                    float x = z[u][i] * mod.scale;
-                    if (mod.cap > 0.f) x = mod.cap * tanhf(x * mod.inv_cap);  // tanhf: the scores' errors are the weights' relative errors
-                    if (mod.slopes) x -= slope * fabsf(pos_t - (pos ? (float)pos[min(key, Tn - 1)] : (float)key));
+                    float x = capped_score(z[u][i], mod.scale, mod.cap, mod.inv_cap);
+                    if (mod.slopes) x -= slope * fabsf(pos_t - (float)pos_k[u][i]);
                     z[u][i] = key >= lim ? -INFINITY : x * kLog2e;
                 } else if (key > q0 + lr) {
                     z[u][i] = -INFINITY;
