@@ -364,9 +364,9 @@ int dec_combine(const DecCall &a, const DecWs &ws, int nsplit, hipStream_t st) {
 }
 
 size_t attn_decode_cache_ws(int T, int Hq, int Hkv, int d, bool kv4, bool weights, strd_dtype io) {
-    // (a plain cache that 16-byte reads do not fit takes the general kernel whatever its shape: room for either's splits)
+    // (a query or a plain cache that 16-byte reads do not fit takes the general kernel whatever its shape: room for either's splits)
     int tps, n = dec_splits_general(T, Hq, Hkv, tps);
-    if (dec_mfma_supported(T, Hq, Hkv, d, kv4, io)) n = kv4 ? dec_mfma_splits(T, Hkv, d, kv4, tps) : max(n, dec_mfma_splits(T, Hkv, d, kv4, tps));
+    if (dec_mfma_supported(T, Hq, Hkv, d, kv4, io)) n = max(n, dec_mfma_splits(T, Hkv, d, kv4, tps));
     return dec_ws_bytes(n, Hq, d, dec_ldt(T), weights);
 }
 

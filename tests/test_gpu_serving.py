@@ -339,6 +339,31 @@ def test_decode_spread_scores(d, dtype, kv4):
     _decode_check(q, k, v, sl, ps, w, 0.0, kv4)
 
 
+@pytest.mark.parametrize("T,Hq,Hkv,d", [(843, 32, 8, 128), (2000, 8, 2, 64), (33, 4, 4, 128)])
+@pytest.mark.parametrize("kv4", [True, False])
+def test_decode_takes_a_query_that_wide_reads_do_not_fit(T, Hq, Hkv, d, kv4):
+    """It runs on the other kernel, whose shares of the cache are others, in the same workspace (and not behind it)."""
+    _say("odd query", T, Hq, Hkv, d, kv4)
+    q, k, v, sl, ps, w = _decode_case(T, Hq, Hkv, d, BF16, kv4, True, True)
+    wide = torch.zeros(Hq * d + 8, dtype=BF16, device=DEV)
+    odd = wide[1:1 + Hq * d].view(Hq, d)
+    odd.copy_(q)
+    c = _cache(T, Hkv, d)
+    strd.kv4_store(_dev(k), _dev(v), c, 0)
+    need = (strd.binding.lib().strd_attn_decode_step_kv4_workspace if kv4 else strd.binding.lib().strd_attn_decode_step_weights_workspace)(T, Hq, Hkv, d, 1, 1)
+    room = torch.full((need + 4096,), 0x5A, dtype=torch.uint8, device=DEV)
+    more = dict(cap=20.0, slopes=_dev(sl), pos=_dev(ps), weights=_dev(w), ws=room[:need])
+    o, got = strd.attn_decode_step_kv4(odd, c, T, **more) if kv4 else strd.attn_decode_step_weights(odd, _dev(k), _dev(v), **more)
+    kk, vv, part = np64(k), np64(v), np.zeros(1)
+    if kv4:
+        kk = plain.kv4_values(*plain.kv4_quantize(k.float().numpy()))[0].astype(np.float64)
+        vv, part = (a.astype(np.float64) for a in plain.kv4_values(*plain.kv4_quantize(v.float().numpy())))
+    want, ww, es, mag, ew = plain.decode(np64(q), kk, vv, 20.0, np64(sl), ps.numpy(), np64(w), vmag=np.abs(part) + np.abs(vv))
+    _within(o, want, _out_bound(want, es, mag, BF16, min(T, 512)), "o")
+    _within(got, ww, ew + min(T, 512) * plain.U32 * np.abs(ww) + 1e-30, "weights")
+    assert (room[need:] == 0x5A).all()
+
+
 @pytest.mark.parametrize("cap", [1e-38, 1e7, 3e38])
 @pytest.mark.parametrize("d,dtype", [(64, BF16), (128, BF16), (96, BF16), (128, F32)])
 def test_decode_caps_far_from_the_scores(cap, d, dtype):

@@ -121,6 +121,16 @@ def test_workspaces_follow_the_sizes():
     assert L.strd_cache_evict_workspace(10, 11, 0, 0) == 0
 
 
+def test_workspaces_have_room_for_either_kernel():
+    """Whether the query's address allows wide reads is not known when the workspace is asked for: fp32 names the other kernel's need."""
+    L = binding.lib()
+    for fn in (L.strd_attn_decode_step_kv4_workspace, L.strd_attn_decode_step_weights_workspace):
+        for T in (31, 32, 33, 200, 843, 2000, 8491, 131627, 10 ** 6):
+            for Hq, Hkv, d in ((32, 8, 128), (28, 4, 64), (8, 8, 64), (16, 1, 128), (7, 1, 64), (2, 2, 96)):
+                for weights in (0, 1):
+                    assert fn(T, Hq, Hkv, d, weights, BF16) >= fn(T, Hq, Hkv, d, weights, 0), (T, Hq, Hkv, d)
+
+
 def test_kernel_paths():
     L = binding.lib()
     path = lambda *a: L.strd_attn_prefill_varlen_kernel_path(*a)
