@@ -276,15 +276,8 @@ __global__ __launch_bounds__(kWaves * kWave) __attribute__((amdgpu_waves_per_eu(
                 for (int u = 0; u < 2; ++u)
 #pragma unroll
                     for (int k = 0; k < RL; ++k) far = fmaxf(far, fabsf(pr[p][u][k]));
-            if (__any(far > 0.5f)) {
-#pragma unroll
-                for (int p = 0; p < NP; ++p)
-#pragma unroll
-                    for (int u = 0; u < 2; ++u)
-#pragma unroll
-                        for (int k = 0; k < RL; ++k) pr[p][u][k] = cap2 * tanhf(pr[p][u][k]);
-            } else {
-                // tanh(y) / y up to y = 0.5, as a polynomial in y^2 of least relative error (1.3e-8)
+            // tanh(y) / y up to y = 0.5, as a polynomial in y^2 of least relative error (1.3e-8)
+            auto capped = [&](auto beyond) __attribute__((always_inline)) {
 #pragma unroll
                 for (int p = 0; p < NP; ++p)
 #pragma unroll
@@ -297,8 +290,11 @@ __global__ __launch_bounds__(kWaves * kWave) __attribute__((amdgpu_waves_per_eu(
                             r = fmaf(w, r, -0.333330689f);
                             r = fmaf(w, r, 0.999999987f);
                             pr[p][u][k] = cap2 * y * r;
+                            if constexpr (beyond) pr[p][u][k] = fabsf(y) <= 0.5f ? pr[p][u][k] : cap2 * tanhf(y);
                         }
-            }
+            };
+            if (__any(far > 0.5f)) capped(std::true_type());
+            else capped(std::false_type());
         }
         if constexpr (BIAS) {
 #pragma unroll

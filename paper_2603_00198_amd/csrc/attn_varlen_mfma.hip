@@ -4,13 +4,14 @@
 //  * Blocks are dealt by level over the sequences (AttnTab), the longest first; rows have pitches.
 //  * A row sees the keys before its limit: its own number + 1, or its sequence's vision rows.  Limits never fall from one row to
 //    the next, so a wave meets at most two 32-key blocks that only some of its rows see.
-//  * A score becomes cap * tanh(score / cap): where the scores of a block are up to cap / 4, a polynomial in the square that takes
-//    three more instructions than a score without, up to cap / 2 four, else c - 2 c / (2^(score * 2 log2 e / cap) + 1) in units of log2 e, with two
-//    transcendental instructions of a quarter's rate beside the softmax's one.  The bias takes the rows' positions from LDS, where they lie as fp32 numbers beside the keys.
+//  * A score becomes cap * tanh(score / cap): up to cap / 4 by a polynomial in the square that takes three more instructions than a
+//    score without, up to cap / 2 by one of four, and where a row sees more than that in a block, as c - 2 c / (2^(score * 2 log2 e / cap) + 1)
+//    in units of log2 e, with two transcendental instructions of a quarter's rate beside the softmax's one.  What no row of a wave needs is not computed.
+//    The bias takes the rows' positions from LDS, where they lie as fp32 numbers beside the keys.
 //  * What a row does not see does not reach it.  A probability of 0 takes a value out of the second product only if it is finite: in
 //    chunks with hidden keys the values are looked at when they have landed in LDS, and those that are not finite are taken out and
-//    added at the end, row by row.  And a row's softmax reference moves by the row's own scores alone, never because of a neighbour in its wave: a row's
-//    result has the same bits whatever else is in the batch.
+//    added at the end, row by row.  And a row's softmax reference moves by the row's own scores alone, never because of a neighbour in its wave: its
+//    result has the same bits whatever the rows that it does not see hold.
 #include "attn_varlen.h"
 
 namespace strd {
@@ -49,6 +50,10 @@ __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
 }
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ float quarters_max(float v) {  // over the four lanes 16 apart
+    v = fmaxf(v, __shfl_xor(v, 16, kWave));
+    return fmaxf(v, __shfl_xor(v, 32, kWave));
+}
 
 // Takes the elements that are not finite out of the slots of a tile that this lane has copied (and that have landed); whether
 // there were any, in any lane of the wave.
@@ -278,53 +283,59 @@ __global__ __launch_bounds__((G * NW + NC) * kWave) __attribute__((amdgpu_waves_
                 // the transposed V fragments are requested now and arrive during the softmax: lane group lb
                 // passes rows 4 lb + lr / 4 (then + 16) and columns 4 (lr % 4) of a 16-channel tile and
                 // receives, for channel lr, the keys 4 lb .. 4 lb + 3 (then 16 + 4 lb ..): the slot order of P
-                // (64 channels now -- with a bias once it is in, its registers are needed until then; the other 64 are requested after the
+                // (64 channels now -- with a cap or a bias once it is in, their registers are needed until then; the other 64 are requested after the
                 // softmax, when the score registers are free)
                 strd_s16x4 vr8[DT / 4][8];
                 const bf16_t *vp = lds.v[cur].at(32 * kt + 4 * lb + (lr >> 2), 4 * (lr & 3));
-                if constexpr (!BIAS)
+                if constexpr (!CAP && !BIAS)
                     lds_issue_tr8<0, 16 * kRowB, 32, 16 * kRowB + 32, 64, 16 * kRowB + 64, 96, 16 * kRowB + 96>(vp, vr8[0]);
+                const bool edge = kb + 32 > wlo;  // uniform: some (key, query) pair of the block is masked
+                auto hide_scores = [&](float with) __attribute__((always_inline)) {
+                    // (hides the row: keeps this a branch -- folded into selects it would run for every block -- and the limits out of registers)
+                    int first = row(0);
+                    asm volatile("" : "+v"(first));
+                    const int lim[2] = {limit(first), limit(first + 16)};
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const int key = kb + 16 * j + 4 * lb + r;
+                            if (key >= lim[0]) sacc[0][j][r] = with;
+                            if (key >= lim[1]) sacc[1][j][r] = with;
+                        }
+                };
                 if constexpr (CAP) {
                     // (less the row's reference, added in the same instruction: the exponents as they are, unless the reference moves)
-                    float far = 0.f;
-#pragma unroll
-                    for (int qt = 0; qt < 2; ++qt)
-#pragma unroll
-                        for (int j = 0; j < 2; ++j)
-#pragma unroll
-                            for (int r = 0; r < 4; ++r) far = fmaxf(far, fabsf(sacc[qt][j][r]));
-                    if (__builtin_expect(__any(far > pr.near), 0)) {
-                        if (__any(far > pr.half)) {
-#pragma unroll
-                            for (int qt = 0; qt < 2; ++qt) {
-                                const float top = pr.c2 + m_neg[qt];
-#pragma unroll
-                                for (int j = 0; j < 2; ++j)
-#pragma unroll
-                                    for (int r = 0; r < 4; ++r)
-                                        sacc[qt][j][r] = fmaf(pr.c2_twice, __builtin_amdgcn_rcpf(ex2(sacc[qt][j][r] * pr.kappa) + 1.f), top);
-                            }
-                        } else {
-#pragma unroll
-                            for (int qt = 0; qt < 2; ++qt)
-#pragma unroll
-                                for (int j = 0; j < 2; ++j)
-#pragma unroll
-                                    for (int r = 0; r < 4; ++r) {
-                                        const float y = sacc[qt][j][r], w = y * y;
-                                        sacc[qt][j][r] = fmaf(y, fmaf(w, fmaf(w, fmaf(w, pr.tanh_half[3], pr.tanh_half[2]), pr.tanh_half[1]), pr.tanh_half[0]), m_neg[qt]);
-                                    }
-                        }
-                    } else {
+                    auto each = [&](auto form) __attribute__((always_inline)) {
 #pragma unroll
                         for (int qt = 0; qt < 2; ++qt)
 #pragma unroll
                             for (int j = 0; j < 2; ++j)
 #pragma unroll
-                                for (int r = 0; r < 4; ++r) {
-                                    const float y = sacc[qt][j][r], w = y * y;
-                                    sacc[qt][j][r] = fmaf(y, fmaf(w, fmaf(w, pr.tanh_near[2], pr.tanh_near[1]), pr.tanh_near[0]), m_neg[qt]);
-                                }
+                                for (int r = 0; r < 4; ++r) sacc[qt][j][r] = form(qt, sacc[qt][j][r]);
+                    };
+                    auto near = [&](float w) { return fmaf(w, fmaf(w, pr.tanh_near[2], pr.tanh_near[1]), pr.tanh_near[0]); };
+                    auto half = [&](int qt, float y) {
+                        const float w = y * y, h = fmaf(w, fmaf(w, fmaf(w, pr.tanh_half[3], pr.tanh_half[2]), pr.tanh_half[1]), pr.tanh_half[0]);
+                        return fmaf(y, fabsf(y) <= pr.near ? near(w) : h, m_neg[qt]);
+                    };
+                    auto any = [&](int qt, float y) { return fmaf(pr.c2_twice, __builtin_amdgcn_rcpf(ex2(y * pr.kappa) + 1.f), pr.c2 + m_neg[qt]); };
+                    if (BIAS && edge) hide_scores(0.f);  // (here for registers' sake, else below)
+                    float far = 0.f;
+                    each([&](int, float y) { far = fmaxf(far, fabsf(y)); return y; });
+                    if (__builtin_expect(!__any(far > pr.near), 1)) {
+                        each([&](int qt, float y) { return fmaf(y, near(y * y), m_neg[qt]); });
+                    } else if (!__any(far > pr.half)) {
+                        each(half);
+                    } else {
+                        // What a row sees of the block decides for all of it, so that nothing else has a part in its bits; where every row takes the
+                        // exponential form, nothing else is computed.
+                        if (!BIAS && edge) hide_scores(0.f);
+                        float top[2] = {0.f, 0.f};
+                        each([&](int qt, float y) { top[qt] = fmaxf(top[qt], fabsf(y)); return y; });
+                        top[0] = quarters_max(top[0]), top[1] = quarters_max(top[1]);
+                        if (__any(fminf(top[0], top[1]) <= pr.half)) each([&](int qt, float y) { return top[qt] <= pr.half ? half(qt, y) : any(qt, y); });
+                        else each(any);
                     }
                 }
                 if constexpr (BIAS) {
@@ -337,22 +348,8 @@ __global__ __launch_bounds__((G * NW + NC) * kWave) __attribute__((amdgpu_waves_
                             for (int r = 0; r < 4; ++r) sacc[qt][j][r] = fmaf(-slope, fabsf(pk[r] - pos_q[qt]), sacc[qt][j][r]);
                     }
                 }
-                const bool edge = kb + 32 > wlo;  // uniform: some (key, query) pair of the block is masked
-                if (edge) {
-                    // (hides the row: keeps this a branch -- folded into selects it would run for every block -- and the limits out of registers)
-                    int first = row(0);
-                    asm volatile("" : "+v"(first));
-                    const int lim[2] = {limit(first), limit(first + 16)};
-#pragma unroll
-                    for (int j = 0; j < 2; ++j)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            const int key = kb + 16 * j + 4 * lb + r;
-                            if (key >= lim[0]) sacc[0][j][r] = -INFINITY;
-                            if (key >= lim[1]) sacc[1][j][r] = -INFINITY;
-                        }
-                }
-                if constexpr (BIAS)
+                if (edge) hide_scores(-INFINITY);
+                if constexpr (CAP || BIAS)
                     lds_issue_tr8<0, 16 * kRowB, 32, 16 * kRowB + 32, 64, 16 * kRowB + 64, 96, 16 * kRowB + 96>(vp, vr8[0]);
                 // The probabilities, against the reference as it is (of a row that has seen no key yet: 0).  The row sum is taken of
                 // them as they enter the second product, i.e. rounded to bf16 (numerator and denominator then carry the same

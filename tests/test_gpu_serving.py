@@ -106,6 +106,20 @@ def test_prefill_varlen_caps_far_above_the_scores(cap, dtype, d):
     _within(o, want, _out_bound(want, 2 * es, mag, dtype, 230), "o")
 
 
+@pytest.mark.parametrize("dtype,d", [(F32, 64), (BF16, 64), (BF16, 128), (BF16, 96)])
+@pytest.mark.parametrize("cap,slopes", [(0.0, False), (20.0, False), (20.0, True)])
+def test_prefill_varlen_rows_keep_their_bits_whatever_comes_behind_them(cap, slopes, dtype, d):
+    _say("bits", cap, slopes, dtype, d)
+    for seqs, Hq, Hkv in (([(300, 30, 0), (90, 0, 0)], 4, 2), ([(600, 0, 0), (90, 0, 0)], 40, 2), ([(1100, 0, 0), (20, 0, 0)], 80, 8)):
+        q, k, v, sl, _ = _prefill(seqs, Hq, Hkv, d, dtype, cap, slopes, False, False, seed=6)
+        first = strd.attn_prefill_varlen(_dev(q), _dev(k), _dev(v), seqs, cap=cap, slopes=_dev(sl))
+        for at in (135, 200):
+            for x in (q, k, v):
+                x[at:seqs[0][0]] *= 37.0
+            o = strd.attn_prefill_varlen(_dev(q), _dev(k), _dev(v), seqs, cap=cap, slopes=_dev(sl))
+            assert torch.equal(o[:135], first[:135]) and torch.equal(o[seqs[0][0] + seqs[0][1]:], first[seqs[0][0] + seqs[0][1]:])
+
+
 @pytest.mark.parametrize("cap", [1e-38, 1e-3])
 @pytest.mark.parametrize("dtype,d", [(F32, 64), (BF16, 128)])
 def test_prefill_varlen_caps_far_below_the_scores(cap, dtype, d):
@@ -362,6 +376,17 @@ def test_decode_takes_a_query_that_wide_reads_do_not_fit(T, Hq, Hkv, d, kv4):
     _within(o, want, _out_bound(want, es, mag, BF16, min(T, 512)), "o")
     _within(got, ww, ew + min(T, 512) * plain.U32 * np.abs(ww) + 1e-30, "weights")
     assert (room[need:] == 0x5A).all()
+
+
+@pytest.mark.parametrize("d,dtype", [(64, BF16), (128, BF16), (96, BF16), (128, F32)])
+@pytest.mark.parametrize("cap", [0.0, 20.0])
+def test_decode_heads_keep_their_bits_whatever_the_others_do(cap, d, dtype):
+    _say("decode bits", cap, d, dtype)
+    q, k, v, _, _, _ = _decode_case(500, 8, 2, d, dtype, False, False, False)
+    first, _ = strd.attn_decode_step_weights(_dev(q), _dev(k), _dev(v), cap=cap)
+    q[1::2] *= 37.0
+    o, _ = strd.attn_decode_step_weights(_dev(q), _dev(k), _dev(v), cap=cap)
+    assert torch.equal(o[0::2], first[0::2])
 
 
 @pytest.mark.parametrize("cap", [1e-38, 1e7, 3e38])
