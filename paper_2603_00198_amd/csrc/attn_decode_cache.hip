@@ -7,6 +7,7 @@
 // group has a softmax of its own, and the 16 of a workgroup meet in LDS.  Where weights are wanted the scores go to the workspace.
 // Pass 2: a workgroup per 32 output channels of a head joins the splits; others turn the scores of 256 or 512 tokens into weights,
 // once the heads' references and sums over all splits are known: w = w_in + mean over the heads of 2^(score - ref) / sum.
+// Pass 2 is a launch and two round trips to memory, 3.8 us up to some ten thousand tokens, 8.5 at 131627 (17 MB of scores).
 #include "attn_decode_cache.h"
 
 namespace strd {

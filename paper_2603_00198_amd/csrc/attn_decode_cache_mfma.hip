@@ -18,6 +18,8 @@
 // A wave takes 32 rows at a time, the next ones on their way; its softmax has one reference per head that moves when a score is
 // 2^8 above it.  The last rows are read as the last 32 of the cache, those before them masked (their scores are -inf; a row that holds NaN has
 // made the result NaN already), so that no read is clamped.  Weights: the scores go to the workspace as they come.
+// 131627 rows of 8 heads of 128 in 4 bits, 32 query heads, cap, bias and weights: 51 us (170 MB, 3.3 TB/s), the reads alone 37 to 44;
+// 843 rows 6.3 us.  Three trips on their way, or (s, z) read once for the heads and handed round, do not pass this (54 and 52 us).
 #include "attn_decode_cache.h"
 
 namespace strd {

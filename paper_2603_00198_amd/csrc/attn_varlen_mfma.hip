@@ -12,6 +12,10 @@
 //    chunks with hidden keys the values are looked at when they have landed in LDS, and those that are not finite are taken out and
 //    added at the end, row by row.  And a row's softmax reference moves by the row's own scores alone, never because of a neighbour in its wave: its
 //    result has the same bits whatever the rows that it does not see hold.
+// Bound by the matrix products and the vector instructions of a SIMD, which overlap only in part (attn_mfma.hip), and for short
+// batches by the start and end of a workgroup.  us: 8320 tokens, 32 / 8 heads of 128: 490 (1.16 PFLOP/s), biased 519, cap 50 580 to 590, both 643;
+// 2176 tokens, biased 63; six sequences of 3493 tokens, 28 / 4 heads of 64, prefix 41.  A cap of 15 at scores of deviation 1 629, one that
+// every score is beyond 790; where some rows of a wave's blocks are beyond half of it and some not, both forms are computed: twice the time.
 #include "attn_varlen.h"
 
 namespace strd {
@@ -136,7 +140,7 @@ __global__ __launch_bounds__((G * NW + NC) * kWave) __attribute__((amdgpu_waves_
 
     // Chunks in the order they are taken.  With a bias the nearest keys come first, those of the workgroup's own rows and then back to the
     // first, then the ones ahead (a prefix): from far to near the softmax reference would move in every block.  8320 tokens, 32 heads of 128,
-    // slopes up to 1: 846 us in the order of the keys.
+    // slopes up to 1: 519 us, 846 in the order of the keys.
     const int own = min(t0 + kBM, nkeys) - 1, nearest = own / KC;
     auto chunk_at = [&](int i) { return BIAS && i <= nearest ? nearest - i : i; };
 
@@ -549,7 +553,7 @@ int launch_d(Params &pr, const strd_seq *seqs, int nseq, long long blocks128, lo
     const int Hq = pr.Hq;
     const long long wgs128 = blocks128 * Hq, wgs256 = blocks256 * Hq;
     if constexpr (D == 64) {
-        // Four workgroups of four waves fit a CU, and pass one of 256 rows (8320 tokens, 28 heads: 279 / 286 us, with a cap and a bias 410 / 441;
+        // Four workgroups of four waves fit a CU, and pass one of 256 rows (8320 tokens, 28 heads: 279 / 286 us;
         // six sequences of 3493 tokens and a prefix 43 / 50).  Few of them: two groups of waves with a copying one, each on half of the keys (2981
         // tokens, 28 heads 57 / 53 us; 2176 tokens, 32 heads 44 / 40, with a prefix 62 / 66; 3493 tokens in six, 28 heads 31 / 41).
         const bool one = longest <= 256 || wgs128 > (pr.mod.prefix ? 512 : 640 + 4 * blocks128);

@@ -52,7 +52,7 @@ __device__ __forceinline__ uint32_t order_key(float f) {
 
 // A selection that leaves out the first rows, which are kept whatever they score, and those from N on (cache_evict): their
 // slots have key 0 as those past the end, and one workgroup writes their indices around the selected ones.  K and idx are the
-// selection's, idx + K the place of the last rows.
+// selection's, idx + K the place of the last rows.  1075 rows 4.7 us, 8363 10.6, 131627 19, as a selection of as many.
 struct Kept {
     int first, last;
 };
