@@ -204,7 +204,7 @@ __global__ __launch_bounds__(kWaves * kWave) __attribute__((amdgpu_waves_per_eu(
             if constexpr (KV4) z = mfma16(ones, bq[p][i], z);
         }
         qsum[p] = z[0];
-        slope[p] = BIAS && hh < rep ? mod.slopes[hk * rep + hh] * kLog2e : 0.f;
+        slope[p] = BIAS && hh < rep ? fminf(fmaxf(mod.slopes[hk * rep + hh] * kLog2e, -1e30f), 1e30f) : 0.f;  // (infinity times 0 is NaN)
         m[p] = kDecNegBig;
         l[p] = corr[p] = 0.f;
 #pragma unroll

@@ -28,6 +28,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLazy = 8.f;       // log2 of how far a probability may exceed 1 before the reference moves
+constexpr float kLowest = 67108864.f;  // log2 of how far below 1 a probability with a bias is not looked at any more
 constexpr float kLazySum = 256.f;  // the same, of what the probabilities of a lane's 8 keys add up to
 
 // K rows are read 16 bytes per lane, lane = (row lane % 16, piece lane / 16), V with the transposing load,
@@ -231,6 +232,7 @@ __global__ __launch_bounds__((G * NW + NC) * kWave) __attribute__((amdgpu_waves_
     float pos_q[2] = {0.f, 0.f}, slope = 0.f;
     if constexpr (BIAS) {
         slope = CAP ? pr.mod.slopes[h] * kLog2e : pr.mod.slopes[h] / pr.mod.scale;  // in the scores' units
+        slope = fminf(fmaxf(slope, -1e30f), 1e30f);  // (infinity times a distance of 0 is NaN)
         slope = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, slope)));  // (a scalar register)
         pos_q[0] = (float)(pos ? pos[min(row(0), T - 1)] : row(0));
         pos_q[1] = (float)(pos ? pos[min(row(1), T - 1)] : row(1));
@@ -408,7 +410,9 @@ __global__ __launch_bounds__((G * NW + NC) * kWave) __attribute__((amdgpu_waves_
                         why = fmaxf(why, __shfl_xor(why, 32, kWave));
                         const bool own = m_run[qt] == -INFINITY || (kBySum ? why > kLazySum : why > limit_of(qt));
                         // (a row may not see any key of the groups behind the first, whose chunks start later)
-                        const float nm = own ? fmaxf(m_run[qt], CAP ? t - m_neg[qt] : t) : m_run[qt];
+                        float nm = own ? fmaxf(m_run[qt], CAP ? t - m_neg[qt] : t) : m_run[qt];
+                        // (a steep bias: keys so far down give way to the row's own, and as a reference they would be off by more than 2^2)
+                        if (BIAS) nm = nm * scale2 < -kLowest ? -INFINITY : nm;
                         const bool none = nm == -INFINITY;
                         const float corr = none ? 1.f : ex2((m_run[qt] - nm) * scale2);
                         l_run[qt] *= corr;

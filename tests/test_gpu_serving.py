@@ -120,6 +120,23 @@ def test_prefill_varlen_rows_keep_their_bits_whatever_comes_behind_them(cap, slo
             assert torch.equal(o[:135], first[:135]) and torch.equal(o[seqs[0][0] + seqs[0][1]:], first[seqs[0][0] + seqs[0][1]:])
 
 
+@pytest.mark.parametrize("dtype,d", [(F32, 64), (BF16, 64), (BF16, 128), (BF16, 96)])
+@pytest.mark.parametrize("cap", [0.0, 20.0])
+def test_prefill_varlen_steep_biases(cap, dtype, d):
+    """Every key but a row's own far below it, in blocks that are taken before the row's own as well."""
+    _say("steep", cap, dtype, d)
+    for seqs, Hq, Hkv in (([(700, 30, 0), (90, 0, 0)], 4, 2), ([(600, 0, 0)], 40, 2), ([(20, 5, 0), (230, 0, 0)], 5, 1)) + (
+            (([(1100, 0, 0)], 80, 8),) if d == 128 else ()):
+        q, k, v, _, _ = _prefill(seqs, Hq, Hkv, d, dtype, cap, False, False, True, seed=8)
+        sl = torch.tensor([1e3, 1e10, 3e38, 0.0, 1e6])[torch.arange(Hq) % 5]
+        o = strd.attn_prefill_varlen(_dev(q), _dev(k), _dev(v), seqs, prefix=True, cap=cap, slopes=_dev(sl))
+        steep = torch.arange(Hq)[sl > 0]   # exp(-1000) and less is 0: a row's own value is all that is left, with a weight of 1
+        assert torch.equal(o[:, steep.to(DEV)], _dev(v[:, steep // (Hq // Hkv)]))
+        if Hq > 3:
+            want, es, mag = plain.attn_varlen(np64(q[:, 3:4]), np64(k[:, [3 // (Hq // Hkv)]]), np64(v[:, [3 // (Hq // Hkv)]]), seqs, True, cap, None, None)
+            _within(o[:, 3:4], want, _out_bound(want, es, mag, dtype, max(s[0] + s[1] for s in seqs)), "o")
+
+
 @pytest.mark.parametrize("cap", [1e-38, 1e-3])
 @pytest.mark.parametrize("dtype,d", [(F32, 64), (BF16, 128)])
 def test_prefill_varlen_caps_far_below_the_scores(cap, dtype, d):
