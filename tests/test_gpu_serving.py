@@ -550,6 +550,59 @@ def test_prefill_store_decode_evict_together(dtype, d):
             p64, w64, wb = p64[i], w64[i], wb[i]
 
 
+@pytest.mark.parametrize("seed", range(40))
+def test_random_shapes_prefill(seed):
+    rng = np.random.default_rng(seed)
+    Hkv = int(rng.integers(1, 5))
+    Hq, d = Hkv * int(rng.integers(1, 9)), int(rng.choice([64, 128, 64, 128, 96, 40, 160]))
+    dtype = F32 if rng.random() < 0.25 else BF16
+    seqs, left = [], int(2 ** rng.uniform(1, 10.5))
+    while left > 0 and len(seqs) < 16:
+        t = left if rng.random() < 0.3 or len(seqs) == 15 else int(rng.integers(0, left + 1))
+        m = int(rng.integers(0, t + 1)) if rng.random() < 0.3 else int(rng.integers(0, t // 8 + 1))
+        seqs.append((t - m, m, 0))
+        left -= t
+    cap, prefix = float(rng.choice([0.0, 0.0, 1.0, 5.0, 30.0])), bool(rng.random() < 0.5)
+    slopes, pos, pad = bool(rng.random() < 0.5), bool(rng.random() < 0.5), int(rng.choice([0, 0, 8, 3]))
+    _say("random prefill", seed, seqs, Hq, Hkv, d, dtype, cap, prefix, slopes, pos, pad)
+    q, k, v, sl, ps = _prefill(seqs, Hq, Hkv, d, dtype, cap, slopes, pos, prefix, seed=seed)
+    rows = q.shape[0]
+    wide = torch.cat([x.flatten(1) for x in (q, k, v)] + [torch.zeros(rows, pad, dtype=dtype)], 1).to(DEV)
+    parts = [x.unflatten(1, (h, d)) for x, h in zip(wide[:, :(Hq + 2 * Hkv) * d].split([Hq * d, Hkv * d, Hkv * d], 1), (Hq, Hkv, Hkv))]
+    o = strd.attn_prefill_varlen(*parts, seqs, prefix=prefix, cap=cap, slopes=_dev(sl), pos=_dev(ps))
+    want, es, mag = plain.attn_varlen(np64(q), np64(k), np64(v), seqs, prefix, cap, None if sl is None else np64(sl), None if ps is None else ps.numpy())
+    _within(o, want, _out_bound(want, es, mag, dtype, max(s[0] + s[1] for s in seqs)), "o")
+
+
+@pytest.mark.parametrize("seed", range(40))
+def test_random_shapes_decode(seed):
+    rng = np.random.default_rng(100 + seed)
+    Hkv, kv4 = int(rng.integers(1, 10)), bool(rng.random() < 0.6)
+    Hq, d = Hkv * int(rng.integers(1, 13)), int(rng.choice([64, 128, 64, 128, 96, 32, 256] if kv4 else [64, 128, 64, 128, 96, 40, 200]))
+    dtype, T = F32 if rng.random() < 0.25 else BF16, int(2 ** rng.uniform(0, 13))
+    cap, slopes, pos = float(rng.choice([0.0, 0.0, 1.0, 5.0, 30.0])), bool(rng.random() < 0.5), bool(rng.random() < 0.5)
+    _say("random decode", seed, T, Hq, Hkv, d, dtype, kv4, cap, slopes, pos)
+    _decode_check(*_decode_case(T, Hq, Hkv, d, dtype, kv4, slopes, pos, seed=seed), cap, kv4, spare=int(rng.integers(0, 3)))
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_random_shapes_evict(seed):
+    rng = np.random.default_rng(200 + seed)
+    T = int(2 ** rng.uniform(0, 17.5))
+    K = int(rng.integers(1, T + 1))
+    first = int(rng.integers(0, K + 1)) if rng.random() < 0.3 else min(K, int(rng.integers(0, 200)))
+    last = int(rng.integers(0, K - first + 1)) if rng.random() < 0.3 else min(K - first, int(rng.integers(0, 200)))
+    _say("random evict", seed, T, K, first, last)
+    w = torch.from_numpy(rng.random(T).astype(np.float32))
+    if seed % 3 == 0:
+        w = (w * 50).floor()
+    rows, pos = torch.arange(3 * T, dtype=torch.int32).view(T, 3), torch.arange(T, dtype=torch.int32) * 2
+    idx, kw, (out,), kp = strd.cache_evict(_dev(w), K, first, last, [_dev(rows)], pos=_dev(pos))
+    want = torch.from_numpy(plain.evict(w.numpy(), K, first, last))
+    assert torch.equal(idx.cpu().long(), want) and torch.equal(kw.cpu(), w[want]) and torch.equal(kp.cpu(), pos[want])
+    assert torch.equal(out.cpu(), rows[want])
+
+
 def _calls():
     g = torch.Generator().manual_seed(11)
     q, k, v = _rand(g, 200, 8, 64, dtype=BF16).to(DEV), _rand(g, 200, 2, 64, dtype=BF16).to(DEV), _rand(g, 200, 2, 64, dtype=BF16).to(DEV)
