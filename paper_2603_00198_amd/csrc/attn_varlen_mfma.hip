@@ -45,8 +45,12 @@ struct Tile {
     };
     Half k[2];
     Half v[2];
-    float pos[2][KC];  // the keys' positions (only where there is a bias)
-    int odd[8];        // per wave that fills the tiles: whether it has taken values out (the first group's)
+    // In the rows' padding, so that four workgroups of 40 KB fit the LDS (8320 tokens, 28 heads of 64: 286 us with three, 276): the keys'
+    // positions, eight to a row of K (only where there is a bias), ...
+    static_assert((kPitch - D) * sizeof(bf16_t) >= 32, "eight numbers");
+    __device__ __forceinline__ float *pos(int b, int key) { return reinterpret_cast<float *>(k[b].e + (key >> 3) * kPitch + D) + (key & 7); }
+    // ... and per wave that fills the tiles, whether it has taken values out (the first group's).
+    __device__ __forceinline__ int *odd() { return reinterpret_cast<int *>(v[0].e + D); }
 };
 
 __device__ __forceinline__ float ex2(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -185,7 +189,7 @@ __global__ __launch_bounds__((G * NW + NC) * kWave) __attribute__((amdgpu_waves_
         }
         if constexpr (BIAS) {
             static_assert(KC <= (NC ? NC : NW) * kWave, "one position a lane");
-            if (at < KC) dst.pos[b][at] = (float)key_pos;
+            if (at < KC) *dst.pos(b, at) = (float)key_pos;
         }
     };
     // Chunks with keys that not every row of the workgroup sees: values that are not finite are taken out, by the wave that copied
@@ -194,7 +198,7 @@ __global__ __launch_bounds__((G * NW + NC) * kWave) __attribute__((amdgpu_waves_
     bool odd = false;  // uniform
     auto hide = [&](TileT &dst, int chunk, int b) __attribute__((always_inline)) {
         if ((chunk + 1) * KC > wg_lo && chunk < nchunk) odd |= hide_odd<AT>(dst.v[b].e, cw, NC ? NC : NW);
-        if (lane == 0) all[0].odd[grp * NW * (NC == 0) + cw] = odd;
+        if (lane == 0) all[0].odd()[grp * NW * (NC == 0) + cw] = odd;
     };
     static_assert(G == 1 || NC > 0, "a flag per wave that fills tiles");
     if (copies) {
@@ -347,7 +351,7 @@ __global__ __launch_bounds__((G * NW + NC) * kWave) __attribute__((amdgpu_waves_
                 if constexpr (BIAS) {
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
-                        const f32x4 pk = *reinterpret_cast<const f32x4 *>(&lds.pos[cur][32 * kt + 16 * j + 4 * lb]);
+                        const f32x4 pk = *reinterpret_cast<const f32x4 *>(lds.pos(cur, 32 * kt + 16 * j + 4 * lb));
 #pragma unroll
                         for (int qt = 0; qt < 2; ++qt)
 #pragma unroll
@@ -462,7 +466,7 @@ __global__ __launch_bounds__((G * NW + NC) * kWave) __attribute__((amdgpu_waves_
     }
 
 #pragma unroll
-    for (int i = 0; i < (NC ? NC : NW); ++i) odd |= all[0].odd[i] != 0;
+    for (int i = 0; i < (NC ? NC : NW); ++i) odd |= all[0].odd()[i] != 0;
     // this wave's row sums: the four lane groups of a query hold different keys
 #pragma unroll
     for (int qt = 0; qt < 2; ++qt) {
@@ -557,7 +561,7 @@ int launch_d(Params &pr, const strd_seq *seqs, int nseq, long long blocks128, lo
     const int Hq = pr.Hq;
     const long long wgs128 = blocks128 * Hq, wgs256 = blocks256 * Hq;
     if constexpr (D == 64) {
-        // Four workgroups of four waves fit a CU, and pass one of 256 rows (8320 tokens, 28 heads: 279 / 286 us;
+        // Four workgroups of four waves fit a CU, and pass one of 256 rows (8320 tokens, 28 heads: 276 / 286 us;
         // six sequences of 3493 tokens and a prefix 43 / 50).  Few of them: two groups of waves with a copying one, each on half of the keys (2981
         // tokens, 28 heads 57 / 53 us; 2176 tokens, 32 heads 44 / 40, with a prefix 62 / 66; 3493 tokens in six, 28 heads 31 / 41).
         const bool one = longest <= 256 || wgs128 > (pr.mod.prefix ? 512 : 640 + 4 * blocks128);
