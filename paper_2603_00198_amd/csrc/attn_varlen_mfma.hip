@@ -28,7 +28,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLazy = 8.f;       // log2 of how far a probability may exceed 1 before the reference moves
-constexpr float kLowest = 67108864.f;  // log2 of how far below 1 a probability with a bias is not looked at any more
+constexpr float kFar = 1048576.f;  // a softmax reference further from zero than that, in units of log2 e, is taken off the scores themselves
 constexpr float kLazySum = 256.f;  // the same, of what the probabilities of a lane's 8 keys add up to
 
 // K rows are read 16 bytes per lane, lane = (row lane % 16, piece lane / 16), V with the transposing load,
@@ -249,6 +249,12 @@ __global__ __launch_bounds__((G * NW + NC) * kWave) __attribute__((amdgpu_waves_
     // per query tile; l_run: this lane group's share of the row sum
     float m_run[2] = {-INFINITY, -INFINITY}, m_neg[2] = {0.f, 0.f}, l_run[2] = {0.f, 0.f};
     const float scale2 = CAP ? 1.f : pr.scale2, lazy_raw = kLazy / scale2;  // scores' units -> log2
+    // A reference far from zero (large scores; keys ahead under a steep bias) has no place in the instruction that gives an exponent: what is rounded
+    // off it there is half a step of its own size, from 2^26 on a power of two that a sum may not hold.  Such a row's scores are taken less the
+    // reference first, in every block, and 0 is added.  What marks the row makes every block look at the references: with a cap m_neg is 0; without one
+    // m_run is -inf, as before the first key, and m_neg the reference, else 0.  (A flag of the wave beside them: 2 to 4 % slower; so 1 % at most.)
+    auto is_far = [&](float m) { return m > -INFINITY && fabsf(m * scale2) > kFar; };
+    auto reference = [&](int qt) { return CAP || m_run[qt] > -INFINITY || m_neg[qt] == 0.f ? m_run[qt] : m_neg[qt]; };
 
     constexpr int kRowB = TileT::kPitch * 2;  // row pitch of the tiles in bytes
     From from;
@@ -366,14 +372,14 @@ __global__ __launch_bounds__((G * NW + NC) * kWave) __attribute__((amdgpu_waves_
                 // rounding), two at a time.
                 bf16x8 pf[2];
                 float ps[2];
-                auto probabilities = [&]() __attribute__((always_inline)) {
+                auto probabilities = [&](const float (&less)[2]) __attribute__((always_inline)) {
 #pragma unroll
                     for (int qt = 0; qt < 2; ++qt) {
 #pragma unroll
                         for (int j = 0; j < 2; ++j)
 #pragma unroll
                             for (int r = 0; r < 4; ++r)
-                                pf[qt][4 * j + r] = (bf16_t)ex2(CAP ? sacc[qt][j][r] : fmaf(sacc[qt][j][r], scale2, m_neg[qt]));
+                                pf[qt][4 * j + r] = (bf16_t)ex2(CAP ? sacc[qt][j][r] : fmaf(sacc[qt][j][r], scale2, less[qt]));
                         ps[qt] = kBySum ? 0.f : l_run[qt];
 #pragma unroll
                         for (int e = 0; e < 8; e += 2)
@@ -394,47 +400,41 @@ __global__ __launch_bounds__((G * NW + NC) * kWave) __attribute__((amdgpu_waves_
                 // m_run is the reference the exponentials are taken against, common to the four lane groups of a query.  It
                 // follows the running max lazily (attn_mfma.hip): it moves when some lane of the QUERY sees a score more than 2^kLazy above
                 // it, or (kBySum) eight probabilities that add up to more than kLazySum, or the first key.
-                auto limit_of = [&](int qt) { return (CAP ? m_run[qt] + m_neg[qt] : m_run[qt]) + lazy_raw; };  // (of a maximum, -inf before the first key)
+                auto limit_of = [&](int qt) { return CAP ? m_neg[qt] == 0.f ? -INFINITY : lazy_raw : m_run[qt] + lazy_raw; };  // (of a maximum)
                 bool moves;
                 if constexpr (kBySum) {
-                    probabilities();
-                    moves = __any(fmaxf(ps[0], ps[1]) > kLazySum || fminf(m_run[0], m_run[1]) == -INFINITY);
+                    probabilities(m_neg);
+                    moves = __any(fmaxf(ps[0], ps[1]) > kLazySum || (CAP ? m_neg[0] * m_neg[1] == 0.f : fminf(m_run[0], m_run[1]) == -INFINITY));
                     if (moves) maxima();
                 } else {
                     maxima();
                     moves = __any(tm[0] > limit_of(0) || tm[1] > limit_of(1));
                 }
+                float less[2] = {m_neg[0], m_neg[1]};  // (without a cap: what is added to a score in the exponent)
                 if (moves) {
 #pragma unroll
                     for (int qt = 0; qt < 2; ++qt) {
-                        float t = tm[qt], why = kBySum ? ps[qt] : tm[qt];
-                        t = fmaxf(t, __shfl_xor(t, 16, kWave));
-                        t = fmaxf(t, __shfl_xor(t, 32, kWave));
-                        why = fmaxf(why, __shfl_xor(why, 16, kWave));
-                        why = fmaxf(why, __shfl_xor(why, 32, kWave));
-                        const bool own = m_run[qt] == -INFINITY || (kBySum ? why > kLazySum : why > limit_of(qt));
+                        const float t = quarters_max(tm[qt]), why = kBySum ? quarters_max(ps[qt]) : t, old = reference(qt);
+                        const bool own = (CAP ? m_neg[qt] == 0.f : m_run[qt] == -INFINITY) || why > (kBySum ? kLazySum : limit_of(qt));
                         // (a row may not see any key of the groups behind the first, whose chunks start later)
-                        float nm = own ? fmaxf(m_run[qt], CAP ? t - m_neg[qt] : t) : m_run[qt];
-                        // (a steep bias: keys so far down give way to the row's own, and as a reference they would be off by more than 2^2)
-                        if (BIAS) nm = nm * scale2 < -kLowest ? -INFINITY : nm;
-                        const bool none = nm == -INFINITY;
-                        const float corr = none ? 1.f : ex2((m_run[qt] - nm) * scale2);
+                        const float nm = own ? fmaxf(old, CAP ? t - m_neg[qt] : t) : old;
+                        const bool none = nm == -INFINITY, apart = is_far(nm);
+                        const float corr = none ? 1.f : ex2((old - nm) * scale2);
                         l_run[qt] *= corr;
 #pragma unroll
                         for (int dt = 0; dt < DT; ++dt) oacc[dt][qt] *= corr;
-                        m_run[qt] = nm;
-                        const float neg = none ? 0.f : -nm * scale2;
-                        if constexpr (CAP) {
+                        const float neg = none || apart ? 0.f : -nm * scale2, by = (CAP ? neg - m_neg[qt] : 0.f) - (apart ? nm : 0.f);
 #pragma unroll
-                            for (int j = 0; j < 2; ++j)
+                        for (int j = 0; j < 2; ++j)
 #pragma unroll
-                                for (int r = 0; r < 4; ++r) sacc[qt][j][r] += neg - m_neg[qt];
-                        }
-                        m_neg[qt] = neg;
+                            for (int r = 0; r < 4; ++r) sacc[qt][j][r] += by;
+                        m_run[qt] = !CAP && apart ? -INFINITY : nm;
+                        m_neg[qt] = !CAP && apart ? nm : neg;
+                        if constexpr (!CAP) less[qt] = neg;
                     }
-                    if constexpr (kBySum) probabilities();
+                    if constexpr (kBySum) probabilities(less);
                 }
-                if constexpr (!kBySum) probabilities();
+                if constexpr (!kBySum) probabilities(less);
                 l_run[0] = kBySum ? l_run[0] + ps[0] : ps[0];
                 l_run[1] = kBySum ? l_run[1] + ps[1] : ps[1];
 #pragma unroll
@@ -481,6 +481,7 @@ __global__ __launch_bounds__((G * NW + NC) * kWave) __attribute__((amdgpu_waves_
         f32x4 *part = reinterpret_cast<f32x4 *>(smem_raw) + (size_t)w * kPart * kWave + lane;
         static_assert((size_t)NW * kPart * kWave * sizeof(f32x4) <= G * sizeof(TileT), "partials fit the tiles' LDS");
         async_tile_wait();  // (copies past the last chunk)
+        m_run[0] = reference(0), m_run[1] = reference(1);
         __syncthreads();
         if (grp == 1) {
 #pragma unroll
