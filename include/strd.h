@@ -434,7 +434,8 @@ int strd_attn_decode_step(const void *q, const void *k_cache, const void *v_cach
  * channel 2 i in the low half of byte i, channel 2 i + 1 in the high half, and two bf16 numbers s, z; a code stands for
  * z + s (n - 8).  With lo, hi the smallest and the largest of the 32 and fp32 arithmetic: s = bf16((hi - lo) / 15), 0 if below
  * 2^-100; z = bf16(lo + 8 s); n = clamp(rint((x - z) / s) + 8, 0, 15), ties to even.  A value is off by s / 2 and the rounding of s and z
- * at most (|z| 2^-9 + s / 16).  A group with a value that is not finite, or whose s or z is not, reads back as NaN.
+ * at most (|z| 2^-8 + s / 16), where s = 0 by the group's spread too, which is below 2^-96 there.  A group with a value that is not finite,
+ * or whose s or z is not, reads back as NaN.
  *   k_codes, v_codes [dev] [rows, Hkv, d / 2] bytes    k_meta, v_meta [dev] [rows, Hkv, d / 32, 2] bf16 (s, z)
  * all 16-byte aligned (else STRD_EINVAL); d a multiple of 32 up to 256 (else STRD_EUNSUPPORTED).  They compact as any other tensor.
  *   kv4_store: rows row0 .. row0 + R - 1 of the cache from k, v [dev] [R, Hkv, d] with row pitches ldk, ldv (elements); the

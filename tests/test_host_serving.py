@@ -221,3 +221,29 @@ def test_binding_refuses_what_does_not_fit_together():
         with pytest.raises(strd.StrdError):
             call()
             print("case", i, "was taken")
+
+
+def test_the_error_that_the_header_states_for_four_bits_is_the_definitions():
+    """|z| 2^-8 + s / 16 beside s / 2, read from the header: groups of one value take all of the first term (1 + 2^-8 is half a step of
+    bf16 above 1), spread ones the rest."""
+    import os
+    import re
+
+    import numpy as np
+
+    from oracle import serving as plain
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    text = open(os.path.join(root, "include", "strd.h")).read()
+    exponent, part = (int(x) for x in re.search(r"at most \(\|z\| 2\^(-\d+) \+ s / (\d+)\)", text).groups())
+    rng = np.random.default_rng(3)
+    rows = [np.full(32, v) for v in (1 + 2.0 ** -8, -1 - 2.0 ** -8, 1 + 3 * 2.0 ** -8, 3e4 * (1 + 2.0 ** -8))]
+    rows += [size * rng.standard_normal(32) + mean for size in (1.0, 0.1, 1e-3, 30.0) for mean in (0.0, 1.0, -7.0, 300.0) for _ in range(50)]
+    rows += [np.linspace(0.0, 2.0 ** -97, 32)]          # a spread that counts as none
+    x = np.array(rows, np.float32)[:, None]
+    codes, meta = plain.kv4_quantize(x)
+    got, _ = plain.kv4_values(codes, meta)
+    s, z = (np.repeat(meta[..., i], 32, -1).astype(np.float64) for i in (0, 1))
+    off = np.abs(got.astype(np.float64) - x)
+    bound = s / 2 + s / part + np.abs(z) * 2.0 ** exponent + np.where(s == 0, np.ptp(x, axis=-1, keepdims=True).clip(max=2.0 ** -96), 0)
+    assert (off <= bound * (1 + 2.0 ** -12)).all()      # (fp32's own roundings: 2^-24 of z, 2^-16 of its share)
+    assert (off[:2] > 0.99 * bound[:2]).all()           # and no looser than it has to be
