@@ -437,7 +437,8 @@ int strd_attn_decode_step(const void *q, const void *k_cache, const void *v_cach
  * at most (|z| 2^-8 + s / 16), where s = 0 by the group's spread too, which is below 2^-96 there.  A group with a value that is not finite,
  * or whose s or z is not, reads back as NaN.
  *   k_codes, v_codes [dev] [rows, Hkv, d / 2] bytes    k_meta, v_meta [dev] [rows, Hkv, d / 32, 2] bf16 (s, z)
- * all 16-byte aligned (else STRD_EINVAL); d a multiple of 32 up to 256 (else STRD_EUNSUPPORTED).  They compact as any other tensor.
+ * all 16-byte aligned (else STRD_EINVAL); d a multiple of 32 up to 256, Hkv up to 65535 (else STRD_EUNSUPPORTED).  They compact as
+ * any other tensor.
  *   kv4_store: rows row0 .. row0 + R - 1 of the cache from k, v [dev] [R, Hkv, d] with row pitches ldk, ldv (elements); the
  *              other rows are left as they are.  R = 0 allowed.
  *   kv4_load:  k, v [dev] [R, Hkv, d] (contiguous, 32-byte aligned) from rows row0 ..; values rounded once to io.

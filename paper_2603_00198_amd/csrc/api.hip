@@ -550,7 +550,10 @@ bool kv4_ok(const strd_kv4 *c, int rows, int row0, int R, int Hkv, int d, strd_d
     return c && rows >= 0 && row0 >= 0 && R >= 0 && (long long)row0 + R <= rows && rows <= kMostRows && Hkv >= 1 && d >= 1 && io_ok(io) &&
            (R == 0 || (c->k_codes && c->k_meta && c->v_codes && c->v_meta && aligned16(c->k_codes, c->k_meta, c->v_codes, c->v_meta)));
 }
-bool kv4_takes(int R, int Hkv, int d) { return d % kKv4Group == 0 && d <= 256 && (long long)R * Hkv * (d / 8) <= 256LL * 0x7FFFFFFF; }
+// (a row's pieces of 8 channels and the grid are counted in 32 bits)
+bool kv4_takes(int R, int Hkv, int d) {
+    return d % kKv4Group == 0 && d <= 256 && Hkv <= 65535 && (long long)R * Hkv * (d / 8) <= 256LL * 0x7FFFFFFF;
+}
 }  // namespace
 
 int strd_kv4_store(const void *k, int64_t ldk, const void *v, int64_t ldv, const strd_kv4 *cache, int rows, int row0, int R, int Hkv, int d,

@@ -247,3 +247,23 @@ def test_the_error_that_the_header_states_for_four_bits_is_the_definitions():
     bound = s / 2 + s / part + np.abs(z) * 2.0 ** exponent + np.where(s == 0, np.ptp(x, axis=-1, keepdims=True).clip(max=2.0 ** -96), 0)
     assert (off <= bound * (1 + 2.0 ** -12)).all()      # (fp32's own roundings: 2^-24 of z, 2^-16 of its share)
     assert (off[:2] > 0.99 * bound[:2]).all()           # and no looser than it has to be
+
+
+def test_more_kv_heads_than_32_bit_offsets_reach_are_refused():
+    """Both 4-bit calls count a row's pieces of 8 channels in 32 bits; 2^27 heads of 256 channels would wrap to 0 pieces."""
+    _no_gpu()
+    L, (cases, _keep) = binding.lib(), _cases()
+    for name, heads, ch, pitches, rows in (("strd_kv4_store", 8, 9, (1, 3), (5, 6, 7)), ("strd_kv4_load", 6, 7, (), (1, 2, 3))):
+        for Hkv, d in ((1 << 27, 256), (1 << 30, 128), (65536, 32), ((1 << 31) - 1, 64)):
+            for R in (1, 1 << 30):
+                args = list(cases[name][0])
+                args[heads], args[ch] = Hkv, d
+                for i in pitches:
+                    args[i] = Hkv * d
+                args[rows[0]], args[rows[1]], args[rows[2]] = 1 << 30, 0, R
+                assert getattr(L, name)(*args) == EUNSUPPORTED, (name, Hkv, d, R)
+        args = list(cases[name][0])
+        args[heads], args[ch] = 65535, 32
+        for i in pitches:
+            args[i] = 65535 * 32
+        assert getattr(L, name)(*args) == EHIP, name
