@@ -11,10 +11,12 @@
 //    lanes: they exchange their parts so that each ends up with the whole score of one row of the four (two with two groups), whose cap, bias and
 //    exponential only it computes.
 //  * Values: A = the codes of V with the cache's rows as the contraction index, B = p * s -- p comes from the lane that has it with the
-//    multiplication itself -- rounded to bf16, the one rounding of the path beside the output's, for every (head, group).  A lane
-//    collects 8 rows' codes and regroups their halves.  What the 24 too many and z add does not depend on the channel: each lane sums
-//    p z - 24 (the rounded p s) in fp32.  Rows (channels) of the product and columns of another group belong to nobody.
-//  * A plain cache goes the same way without groups: columns are heads, values are regrouped halves.
+//    multiplication itself -- for every (head, group), as two bf16 numbers, its upper 8 bits and the rest, in two products: what is left out is
+//    2^-16 of a weight, where bf16 alone left 2^-8 (a step over 131627 rows 59.4 -> 59.6 us, over 8491 plain ones 11.9 -> 12.0, with 8 heads to a kv head
+//    60.3 -> 64.7).  A lane collects 8 rows' codes and regroups their halves.  What the 24 too many and z add does not depend on the channel: each lane sums
+//    p z - 24 (both parts of p s) in fp32.  Rows (channels) of the product and columns of another group belong to nobody.
+//  * A plain cache goes the same way without groups: columns are heads, values are regrouped halves.  The lower part is 2^-120 at least there, of
+//    the weights' sign: infinity times 0 would be NaN.
 // A wave takes 32 rows at a time, the next ones on their way; its softmax has one reference per head that moves when a score is
 // 2^8 above it.  The last rows are read as the last 32 of the cache, those before them masked (their scores are -inf; a row that holds NaN has
 // made the result NaN already), so that no read is clamped.  Weights: the scores go to the workspace as they come.
@@ -35,6 +37,7 @@ typedef float f32x2u __attribute__((ext_vector_type(2), aligned(4)));
 
 constexpr int kTrip = 32;
 constexpr float kLog2e = 1.4426950408889634f, kLazy = 8.f;
+constexpr float kLeast = 7.52316385e-37f;  // 2^-120: of the lower part of a plain cache's weight
 
 __device__ __forceinline__ float ex2(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
@@ -220,7 +223,7 @@ __global__ __launch_bounds__(kWaves * kWave) __attribute__((amdgpu_waves_per_eu(
     auto fold = [&](int t0, const Rows &x) __attribute__((always_inline)) {
         const int base = min(t0, Tn - kTrip);
         const bool all = base == t0;  // uniform
-        bf16x8 pb[NP];                // p (4 bits: p * s of the column's group) of the 32 rows, the next product's operand
+        bf16x8 pb[NP], pl[NP];        // p (4 bits: p * s of the column's group) of the 32 rows, the next product's operand: upper and lower bits
         float pr[NP][2][RL];
         // ---- scores ----
 #pragma unroll
@@ -335,6 +338,9 @@ __global__ __launch_bounds__(kWaves * kWave) __attribute__((amdgpu_waves_per_eu(
                         }
                     }
         }
+        // halves of two dwords side by side: lo of both, hi of both
+        auto pair_lo = [](uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); };
+        auto pair_hi = [](uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); };
         // ---- softmax ----
         float tm[NP];
         bool moves = false;
@@ -363,7 +369,7 @@ __global__ __launch_bounds__(kWaves * kWave) __attribute__((amdgpu_waves_per_eu(
         }
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
-            uint32_t w[4];
+            uint32_t w[4], wl[4];
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 float e[RL], ps[4];
@@ -390,20 +396,26 @@ __global__ __launch_bounds__(kWaves * kWave) __attribute__((amdgpu_waves_per_eu(
                 of_row(std::integral_constant<int, 1>());
                 of_row(std::integral_constant<int, 2>());
                 of_row(std::integral_constant<int, 3>());
-                w[2 * u] = bf16_pair(ps[0], ps[1]);
-                w[2 * u + 1] = bf16_pair(ps[2], ps[3]);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const uint32_t a = __builtin_bit_cast(uint32_t, ps[2 * i]), b = __builtin_bit_cast(uint32_t, ps[2 * i + 1]);
+                    float la = ps[2 * i] - __builtin_bit_cast(float, a & 0xFFFF0000u), lb = ps[2 * i + 1] - __builtin_bit_cast(float, b & 0xFFFF0000u);
+                    if constexpr (!KV4) la = fmaxf(la, kLeast), lb = fmaxf(lb, kLeast);
+                    w[2 * u + i] = pair_hi(a, b);
+                    wl[2 * u + i] = bf16_pair(la, lb);
+                }
             }
             if constexpr (KV4) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                for (int i = 0; i < 4; ++i) {
                     corr[p] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w[i]), bf16x2{(bf16_t)-24.f, (bf16_t)-24.f}, corr[p], false);
+                    corr[p] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, wl[i]), bf16x2{(bf16_t)-24.f, (bf16_t)-24.f}, corr[p], false);
+                }
             }
             pb[p] = __builtin_bit_cast(bf16x8, u32x4{w[0], w[1], w[2], w[3]});
+            pl[p] = __builtin_bit_cast(bf16x8, u32x4{wl[0], wl[1], wl[2], wl[3]});
         }
         // ---- values ----
-        // halves of two rows' dwords side by side: lo of both, hi of both
-        auto pair_lo = [](uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); };
-        auto pair_hi = [](uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); };
         uint32_t lo[4][VD], hi[4][VD];
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -431,6 +443,8 @@ __global__ __launch_bounds__(kWaves * kWave) __attribute__((amdgpu_waves_per_eu(
                 }
 #pragma unroll
                 for (int p = 0; p < NP; ++p) oacc[p][J] = mfma16(__builtin_bit_cast(bf16x8, a), pb[p], oacc[p][J]);
+#pragma unroll
+                for (int p = 0; p < NP; ++p) oacc[p][J] = mfma16(__builtin_bit_cast(bf16x8, a), pl[p], oacc[p][J]);
             }
         };
         product(std::integral_constant<int, 0>());

@@ -84,3 +84,43 @@ def test_prefill_varlen_rows_beside_one_with_scores_far_from_zero(kernel, prefix
     others[[0, 37, 131]] = False
     assert torch.equal(o[others], first[others])
     assert torch.isfinite(o.float()).all()
+
+
+# ------------------------------------------------------------------ decode steps: weights in full --
+@pytest.mark.parametrize("kv4", [True, False])
+@pytest.mark.parametrize("T,Hq,Hkv,d,dtype", [(100, 8, 2, 128, BF16), (100, 8, 2, 64, BF16), (843, 16, 2, 128, BF16), (843, 32, 2, 64, BF16), (300, 8, 2, 96, BF16),
+                                              (300, 8, 2, 128, F32)])
+def test_decode_rows_of_equal_values_come_out_as_these(T, Hq, Hkv, d, dtype, kv4):
+    """The weights add up to 1 whatever they are: here 7 of 8 are the same number below 1 before they are divided by their sum, which 8 bits would
+    round by up to 2^-8.  Kept to 16 bits or more they are off by 2^-16, 8 steps of the 4-bit cache by 2^-13: values come out exactly, 0 below 2^-12."""
+    base._say("equal values", T, Hq, Hkv, d, dtype, kv4)
+    v = torch.arange(d).remainder(16).float().expand(T, Hkv, d).to(dtype).contiguous()   # (in 4 bits: step 1, middle 8)
+    q, k = torch.zeros(Hq, d, dtype=dtype), torch.zeros(T, Hkv, d, dtype=dtype)
+    k[::8, :, 0] = 1
+    for i in range(24):
+        q[:, 0] = (0.03 * (i + 1) + 0.01 * torch.arange(Hq)) * d ** 0.5
+        if kv4:
+            c = base._cache(T, Hkv, d)
+            strd.kv4_store(base._dev(k), base._dev(v), c, 0)
+            o, w = strd.attn_decode_step_kv4(base._dev(q), c, T)
+        else:
+            o, w = strd.attn_decode_step_weights(base._dev(q), base._dev(k), base._dev(v))
+        o, want = o.float().cpu(), v[0, 0].float().expand(Hq, d)
+        if dtype == BF16:
+            assert torch.equal(o[want > 0], want[want > 0]), i
+        assert (o - want).abs().max() <= 2.0 ** -12, i
+        assert abs(w.double().sum().item() - 1) <= (T + 64) * 2.0 ** -24
+
+
+@pytest.mark.parametrize("T,Hq,Hkv,d", [(100, 8, 2, 128), (843, 16, 2, 64), (100, 8, 2, 96)])
+def test_decode_rows_with_infinite_values(T, Hq, Hkv, d):
+    """Every row has a weight above 0: an infinite value is the result of its channel, of either sign."""
+    base._say("infinite values", T, Hq, Hkv, d)
+    q, k, v, _, _, _ = base._decode_case(T, Hq, Hkv, d, BF16, False, False, False)
+    for at in (0, 17, T - 1):
+        x = v.clone()
+        x[at, :, 3], x[at, :, 40] = float("inf"), -float("inf")
+        o, _ = strd.attn_decode_step_weights(base._dev(q), base._dev(k), base._dev(x))
+        assert (o[:, 3] == float("inf")).all() and (o[:, 40] == -float("inf")).all(), at
+        o[:, 3] = o[:, 40] = 0
+        assert torch.isfinite(o.float()).all()
