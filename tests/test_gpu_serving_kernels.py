@@ -124,3 +124,32 @@ def test_decode_rows_with_infinite_values(T, Hq, Hkv, d):
         assert (o[:, 3] == float("inf")).all() and (o[:, 40] == -float("inf")).all(), at
         o[:, 3] = o[:, 40] = 0
         assert torch.isfinite(o.float()).all()
+
+
+# ------------------------------------------------------------------ the loop in the README ---
+@pytest.mark.parametrize("dtype,d", [(BF16, 128), (BF16, 64), (F32, 96)])
+def test_the_loop_in_the_readme_goes_on_behind_a_full_cache(dtype, d):
+    """As it stands there, over two evictions; the last step against the plain form over the rows that the cache then holds."""
+    import os
+    base._say("readme", dtype, d)
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    block = next(b for b in open(os.path.join(root, "README.md")).read().split("```") if "cache_evict(" in b and b.startswith("python"))
+    g = torch.Generator().manual_seed(d)
+    Hq, Hkv, K0, M0, K1, M1, rows, K, new = 8, 2, 150, 10, 70, 5, 230, 170, 165
+    pos = torch.cat([torch.randperm(4 * n, generator=g)[:n].sort().values for n in (K0 + M0, K1 + M1)]).to(torch.int32)
+    total = K0 + M0 + K1 + M1
+    q, k, v = (base._rand(g, total, h, d, dtype=dtype).to("cuda") for h in (Hq, Hkv, Hkv))
+    tokens = [(base._rand(g, Hq, d, dtype=dtype, size=1.5).to("cuda"), base._rand(g, 1, Hkv, d, dtype=dtype).to("cuda"),
+               base._rand(g, 1, Hkv, d, dtype=dtype).to("cuda"), 1000 + i) for i in range(new)]
+    names = dict(strd=strd, torch=torch, q=q, k=k, v=v, pos=pos.to("cuda"), slopes=base._slopes(Hq).to("cuda"), tokens=tokens, Hq=Hq, Hkv=Hkv, d=d, K0=K0,
+                 M0=M0, K1=K1, M1=M1, rows=rows, K=K)
+    exec(block[len("python"):], names)
+    T, place = names["T"], names["place"].cpu().numpy()
+    assert T == K + (K0 + M0 + new - rows) - (rows - K)      # 70 rows till it is full, 60 more, then what is left
+    assert (np.diff(place[:T]) > 0).all() and place[T - 1] == 1000 + new - 1 and (place[:4] == pos[:4].numpy()).all()
+    held = [t[:T].cpu() for t in names["cache"]]
+    (kk, _), (vv, part) = (plain.kv4_values(codes.numpy(), meta.float().numpy()) for codes, meta in (held[:2], held[2:]))
+    want, _, es, mag, _ = plain.decode(np64(tokens[-1][0]), kk.astype(float), vv.astype(float), 50.0, np64(base._slopes(Hq)), place[:T],
+                                       vmag=np.abs(part) + np.abs(vv))
+    base._within(names["o1"], want, base._out_bound(want, es, mag, dtype, T), "o1")
+    assert (names["w"][:T] > 0).all() and (names["w"][T:] == 0).all()
