@@ -2,7 +2,7 @@
 // every row has gathered (the cap, the bias and the weights: strd.h).  Any head size up to 256, any number of heads, fp32
 // arithmetic; the shapes of attn_decode_cache_mfma.hip run there.
 //
-// Pass 1: a workgroup takes one kv head's share of the tokens, and up to 8 of its query heads.  16 lanes hold a token's
+// Pass 1: a workgroup takes one kv head's share of the tokens, and up to 4 of its query heads (more: the cache is read again).  16 lanes hold a token's
 // row, 8 neighbouring channels each (two such pieces above 128 channels), and 4 tokens are on their way together; a lane
 // group has a softmax of its own, and the 16 of a workgroup meet in LDS.  Where weights are wanted the scores go to the workspace.
 // Pass 2: a workgroup per 32 output channels of a head joins the splits; others turn the scores of 256 or 512 tokens into weights,
