@@ -153,3 +153,92 @@ def test_the_loop_in_the_readme_goes_on_behind_a_full_cache(dtype, d):
                                        vmag=np.abs(part) + np.abs(vv))
     base._within(names["o1"], want, base._out_bound(want, es, mag, dtype, T), "o1")
     assert (names["w"][:T] > 0).all() and (names["w"][T:] == 0).all()
+
+
+# ------------------------------------------------------------------ every kernel against the plain forms --
+def _heads(Hq, Hkv, some=5):
+    """Some query heads and their kv heads, the first and the last among them."""
+    h = np.unique(np.linspace(0, Hq - 1, min(some, Hq)).astype(int))
+    return h, h // (Hq // Hkv)
+
+
+def _plain_prefill(q, k, v, seqs, prefix, cap, sl, ps, heads, kv):
+    """The plain form of some query heads, one kv head to each."""
+    return plain.attn_varlen(np64(q[:, heads]), np64(k[:, kv]), np64(v[:, kv]), seqs, prefix, cap, None if sl is None else np64(sl[heads]),
+                             None if ps is None else ps.numpy())
+
+
+@pytest.mark.parametrize("kernel,prefix", _prefill_kernels())
+@pytest.mark.parametrize("cap,slopes,pos", [(0.0, False, False), (20.0, False, False), (0.0, True, True), (2.0, True, False)])
+def test_prefill_varlen_every_kernel(kernel, prefix, cap, slopes, pos):
+    dtype, d, seqs, Hq, Hkv, _ = PREFILL[kernel]
+    base._say("every prefill kernel", kernel, prefix, cap, slopes, pos)
+    q, k, v, sl, ps = base._prefill(seqs, Hq, Hkv, d, dtype, cap, slopes, pos, prefix, seed=11)
+    o = strd.attn_prefill_varlen(base._dev(q), base._dev(k), base._dev(v), seqs, prefix=prefix, cap=cap, slopes=base._dev(sl), pos=base._dev(ps))
+    heads, kv = _heads(Hq, Hkv)
+    want, es, mag = _plain_prefill(q, k, v, seqs, prefix, cap, sl, ps, heads, kv)
+    base._within(o[:, heads], want, base._out_bound(want, es, mag, dtype, max(s[0] + s[1] for s in seqs)), "o")
+
+
+@pytest.mark.parametrize("kernel,prefix", _prefill_kernels())
+def test_prefill_varlen_every_kernel_spread_scores(kernel, prefix):
+    """References that move from tile to tile; a bias that is steep, none, one that favours what is far."""
+    dtype, d, seqs, Hq, Hkv, _ = PREFILL[kernel]
+    base._say("spread, every kernel", kernel, prefix)
+    q, k, v, _, _ = base._prefill(seqs, Hq, Hkv, d, dtype, 0.0, False, False, prefix, seed=12, size=8.0)
+    k *= torch.linspace(0.2, 2.0, k.shape[0])[:, None, None].to(dtype)
+    heads, kv = _heads(Hq, Hkv)
+    for sl in (None, torch.tensor([30.0, 0.0, -0.02, 2.0, 1e7])[torch.arange(Hq) % 5]):
+        o = strd.attn_prefill_varlen(base._dev(q), base._dev(k), base._dev(v), seqs, prefix=prefix, slopes=base._dev(sl))
+        want, es, mag = _plain_prefill(q, k, v, seqs, prefix, 0.0, sl, None, heads, kv)
+        base._within(o[:, heads], want, base._out_bound(want, es, mag, dtype, max(s[0] + s[1] for s in seqs)), "o")
+
+
+@pytest.mark.parametrize("kernel,prefix", _prefill_kernels())
+@pytest.mark.parametrize("cap,slopes", [(0.0, False), (20.0, True)])
+def test_prefill_varlen_every_kernel_hides_what_is_not_finite(kernel, prefix, cap, slopes):
+    """Keys and values that are not finite, near the ends of tiles, blocks and sequences: rows that do not see them keep their bits, and a value shows
+    in its channel of the rows that see it, in no other."""
+    dtype, d, seqs, Hq, Hkv, _ = PREFILL[kernel]
+    base._say("not finite, every kernel", kernel, prefix, cap, slopes)
+    q, k, v, sl, _ = base._prefill(seqs, Hq, Hkv, d, dtype, cap, slopes, False, prefix, seed=13)
+    call = lambda kk, vv: strd.attn_prefill_varlen(base._dev(q), base._dev(kk), base._dev(vv), seqs, prefix=prefix, cap=cap, slopes=base._dev(sl)).cpu()
+    first, sees, rows = call(k, v), _sees(seqs, prefix), q.shape[0]
+    n, m = seqs[0][0], seqs[0][1]
+    for at in sorted({0, 31, 63, 64, n - 1, n, n + m - 1, n + m, rows - 1} | ({127, 128, 255, 300} if n > 300 else set()) | ({511, 512, 1000} if n > 1000 else set())):
+        for which, bad in (("k", float("nan")), ("k", float("inf")), ("v", float("nan")), ("v", -float("inf"))):
+            kk, vv = k.clone(), v.clone()
+            (kk if which == "k" else vv)[at, :, ::3] = bad
+            o = call(kk, vv)
+            hidden = torch.from_numpy(~sees[:, at])
+            assert torch.equal(o[hidden], first[hidden]), (at, which, bad)
+            if which == "v":
+                assert not torch.isfinite(o[~hidden][:, :, ::3].float()).any(), (at, which, bad)
+                assert torch.equal(o[~hidden][:, :, 1::3], first[~hidden][:, :, 1::3]), (at, which, bad)
+
+
+# Caches long enough for workgroups that fill a CU (16 MB of keys and values: 13.4 million elements of a side in 4 bits, 4.2 million in bf16), not
+# multiples of a trip: 4, 2 and 1 kv heads of a workgroup, one and two sets of query heads.
+LONG = [(13141, 32, 8, 128, True), (13141, 64, 8, 128, True), (52453, 8, 2, 128, True), (52453, 12, 2, 128, True), (34977, 3, 3, 128, True), (34977, 21, 3, 128, True),
+        (52453, 8, 4, 64, True), (52453, 40, 4, 64, True), (69931, 9, 3, 64, True), (4123, 32, 8, 128, False), (8231, 64, 4, 128, False), (10947, 6, 3, 128, False),
+        (16423, 28, 4, 64, False), (65575, 16, 1, 64, False), (65575, 2, 1, 64, False)]
+
+
+@pytest.mark.parametrize("T,Hq,Hkv,d,kv4", LONG)
+def test_decode_steps_every_long_kernel(T, Hq, Hkv, d, kv4):
+    """With a cap and a bias and with neither.  (More than 65536 tokens: two blocks of weights to a workgroup.)"""
+    base._say("long decode", T, Hq, Hkv, d, kv4)
+    q, k, v, sl, ps, w = base._decode_case(T, Hq, Hkv, d, BF16, kv4, True, True)
+    kk, vv, part = np64(k), np64(v), np.zeros(1)
+    if kv4:
+        cache = base._cache(T + 3, Hkv, d, 0xFF)   # rows behind T hold NaN
+        strd.kv4_store(base._dev(k), base._dev(v), cache, 0)
+        held = [t[:T].cpu() for t in cache]
+        (kk, _), (vv, part) = (tuple(x.astype(np.float64) for x in plain.kv4_values(a.numpy(), b.float().numpy())) for a, b in (held[:2], held[2:]))
+    for cap, bias in ((30.0, True), (0.0, False)):
+        more = dict(cap=cap, slopes=base._dev(sl) if bias else None, pos=base._dev(ps), weights=base._dev(w))
+        o, got = strd.attn_decode_step_kv4(base._dev(q), cache, T, **more) if kv4 else strd.attn_decode_step_weights(base._dev(q), base._dev(k), base._dev(v), **more)
+        want, ww, es, mag, ew = plain.decode(np64(q), kk, vv, cap, np64(sl) if bias else None, ps.numpy(), np64(w), vmag=np.abs(part) + np.abs(vv))
+        # (a sum of T products goes through chains of a few hundred: of a wave's trips, the waves, the splits)
+        base._within(o, want, base._out_bound(want, es, mag, BF16, 1024), "o")
+        base._within(got, ww, ew + 512 * plain.U32 * np.abs(ww) + 1e-30, "weights")
