@@ -242,3 +242,25 @@ def test_decode_steps_every_long_kernel(T, Hq, Hkv, d, kv4):
         # (a sum of T products goes through chains of a few hundred: of a wave's trips, the waves, the splits)
         base._within(o, want, base._out_bound(want, es, mag, BF16, 1024), "o")
         base._within(got, ww, ew + 512 * plain.U32 * np.abs(ww) + 1e-30, "weights")
+
+
+# ------------------------------------------------------------------ values near the end of fp32's range --
+@pytest.mark.parametrize("kernel", ["64 two groups", "128 two groups", "128 eight waves, prefix", "tiles", "tiles fp32"])
+def test_prefill_varlen_values_up_to_the_size_that_the_header_names(kernel):
+    dtype, d, seqs, Hq, Hkv, prefix = PREFILL[kernel]
+    base._say("large values", kernel)
+    q, k, v, _, _ = base._prefill(seqs, Hq, Hkv, d, dtype, 0.0, False, False, bool(prefix), seed=14, size=4.0)
+    v = (v / v.abs().max() * (2.0 ** 111 / (seqs[0][0] + seqs[0][1]))).to(dtype)
+    o = strd.attn_prefill_varlen(base._dev(q), base._dev(k), base._dev(v), seqs, prefix=bool(prefix))
+    heads, kv = _heads(Hq, Hkv)
+    want, es, mag = _plain_prefill(q, k, v, seqs, bool(prefix), 0.0, None, None, heads, kv)
+    base._within(o[:, heads], want, base._out_bound(want, es, mag, dtype, seqs[0][0] + seqs[0][1]), "o")
+
+
+@pytest.mark.parametrize("kv4", [True, False])
+@pytest.mark.parametrize("d,dtype", [(64, BF16), (128, BF16), (96, BF16), (128, F32)])
+def test_decode_values_up_to_the_size_that_the_header_names(d, dtype, kv4):
+    base._say("large values", d, dtype, kv4)
+    q, k, v, _, _, w = base._decode_case(500, 8, 2, d, dtype, kv4, False, False, size=4.0)
+    v = (v / v.abs().max() * (2.0 ** 111 / 500)).to(dtype)
+    base._decode_check(q, k, v, None, None, w, 0.0, kv4)
