@@ -15,8 +15,8 @@
 //    2^-16 of a weight, where bf16 alone left 2^-8 (a step over 131627 rows 59.4 -> 59.6 us, over 8491 plain ones 11.9 -> 12.0, with 8 heads to a kv head
 //    60.3 -> 64.7).  A lane collects 8 rows' codes and regroups their halves.  What the 24 too many and z add does not depend on the channel: each lane sums
 //    p z - 24 (both parts of p s) in fp32.  Rows (channels) of the product and columns of another group belong to nobody.
-//  * A plain cache goes the same way without groups: columns are heads, values are regrouped halves.  The lower part is 2^-120 at least there, of
-//    the weights' sign: infinity times 0 would be NaN.
+//  * A plain cache goes the same way without groups: columns are heads, values are regrouped halves.  The lower part is 2^-24 of the weight
+//    at least there: where it is 0 an infinite value would become NaN.
 // A wave takes 32 rows at a time, the next ones on their way; its softmax has one reference per head that moves when a score is
 // 2^8 above it.  The last rows are read as the last 32 of the cache, those before them masked (their scores are -inf; a row that holds NaN has
 // made the result NaN already), so that no read is clamped.  Weights: the scores go to the workspace as they come.
@@ -37,7 +37,7 @@ typedef float f32x2u __attribute__((ext_vector_type(2), aligned(4)));
 
 constexpr int kTrip = 32;
 constexpr float kLog2e = 1.4426950408889634f, kLazy = 8.f;
-constexpr float kLeast = 7.52316385e-37f;  // 2^-120: of the lower part of a plain cache's weight
+constexpr float kLeast = 0x1p-24f;  // least share of the lower part in a plain cache's weight
 
 __device__ __forceinline__ float ex2(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
@@ -400,7 +400,7 @@ __global__ __launch_bounds__(kWaves * kWave) __attribute__((amdgpu_waves_per_eu(
                 for (int i = 0; i < 2; ++i) {
                     const uint32_t a = __builtin_bit_cast(uint32_t, ps[2 * i]), b = __builtin_bit_cast(uint32_t, ps[2 * i + 1]);
                     float la = ps[2 * i] - __builtin_bit_cast(float, a & 0xFFFF0000u), lb = ps[2 * i + 1] - __builtin_bit_cast(float, b & 0xFFFF0000u);
-                    if constexpr (!KV4) la = fmaxf(la, kLeast), lb = fmaxf(lb, kLeast);
+                    if constexpr (!KV4) la = fmaxf(la, kLeast * ps[2 * i]), lb = fmaxf(lb, kLeast * ps[2 * i + 1]);
                     w[2 * u + i] = pair_hi(a, b);
                     wl[2 * u + i] = bf16_pair(la, lb);
                 }

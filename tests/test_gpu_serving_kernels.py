@@ -264,3 +264,40 @@ def test_decode_values_up_to_the_size_that_the_header_names(d, dtype, kv4):
     q, k, v, _, _, w = base._decode_case(500, 8, 2, d, dtype, kv4, False, False, size=4.0)
     v = (v / v.abs().max() * (2.0 ** 111 / 500)).to(dtype)
     base._decode_check(q, k, v, None, None, w, 0.0, kv4)
+
+
+# ------------------------------------------------------------------ biases that favour what is far --
+@pytest.mark.parametrize("kernel,prefix", _prefill_kernels())
+@pytest.mark.parametrize("cap", [0.0, 20.0])
+def test_prefill_varlen_steep_biases_towards_far_rows(kernel, prefix, cap):
+    """A slope below 0 raises scores with the distance: of 1e3 and more a row the farthest row that is seen takes all, with a weight of 1."""
+    dtype, d, seqs, Hq, Hkv, _ = PREFILL[kernel]
+    base._say("towards far rows", kernel, prefix, cap)
+    q, k, v, _, _ = base._prefill(seqs, Hq, Hkv, d, dtype, cap, False, False, prefix, seed=15)
+    sl = torch.tensor([-1e3, -1e6, -1e12, -1e26])[torch.arange(Hq) % 4]
+    o = strd.attn_prefill_varlen(base._dev(q), base._dev(k), base._dev(v), seqs, prefix=prefix, cap=cap, slopes=base._dev(sl)).cpu()
+    sees, rows = _sees(seqs, prefix), q.shape[0]
+    far = np.where(sees, np.abs(np.arange(rows)[:, None] - np.arange(rows)[None]), -1)
+    one = torch.from_numpy((far == far.max(1, keepdims=True)).sum(1) == 1)   # (in the middle of a prefix there are two)
+    want = v[torch.from_numpy(far.argmax(1))].repeat_interleave(Hq // Hkv, 1)
+    assert torch.equal(o[one], want[one])
+    assert torch.isfinite(o.float()).all()
+
+
+@pytest.mark.parametrize("kv4", [True, False])
+@pytest.mark.parametrize("d,dtype", [(64, BF16), (128, BF16), (96, BF16), (128, F32)])
+def test_decode_steep_biases_either_way(d, dtype, kv4):
+    """The newest row takes all, or the oldest."""
+    base._say("steep decode", d, dtype, kv4)
+    T, Hq, Hkv = 1500, 8, 2
+    q, k, v, _, _, _ = base._decode_case(T, Hq, Hkv, d, dtype, kv4, False, False)
+    v = v.float().mul(4).round().clamp(-8, 7).to(dtype)
+    v[:, :, ::32], v[:, :, 1::32] = -8, 7        # step 1 in 4 bits, middle 0: values are held as they are
+    sl = torch.tensor([-1e3, 1e3, -1e12, 1e12, -1e26, 1e26, 1e6, -1e6])
+    c = base._cache(T, Hkv, d)
+    strd.kv4_store(base._dev(k), base._dev(v), c, 0)
+    o, w = strd.attn_decode_step_kv4(base._dev(q), c, T, slopes=base._dev(sl)) if kv4 else \
+        strd.attn_decode_step_weights(base._dev(q), base._dev(k), base._dev(v), slopes=base._dev(sl))
+    want = torch.stack([v[0 if sl[h] < 0 else T - 1, h // 4] for h in range(Hq)])
+    assert torch.equal(o.cpu(), want)
+    assert w[0] == 0.5 and w[T - 1] == 0.5 and (w[1:T - 1] == 0).all()
