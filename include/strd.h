@@ -416,7 +416,7 @@ int strd_attn_decode_step(const void *q, const void *k_cache, const void *v_cach
  * Scores.  With x = scale * q_t^h . k_j, in this order:
  *     cap > 0:    x = cap * tanh(x / cap)                      (cap = 0: no cap)
  *     slopes:     x = x - slopes[h] * |pos[t] - pos[j]|        (NULL: no bias)
- *   slopes [dev] [Hq] fp32, finite, a negative one times the largest distance above -2^26; pos [dev] int32, a position per row (after a compaction the rows' old
+ *   slopes [dev] [Hq] fp32, finite, a negative one times the largest distance above -1e30; pos [dev] int32, a position per row (after a compaction the rows' old
  *   positions: pos_out of strd_compact), taken as fp32 numbers (exact below 2^24); NULL: the row's number in its sequence.
  * cap must be finite and >= 0, else STRD_EINVAL.
  * Weighted values are summed in fp32 before the sum is divided by that of the weights: a value's size times the number of rows has to stay below 2^112 (5e33).
