@@ -412,7 +412,8 @@ def cache_evict(weights: torch.Tensor, K: int, first: int, last: int, tensors: S
                 pos: Optional[torch.Tensor] = None, outs: Optional[Sequence[torch.Tensor]] = None,
                 ws: Optional[torch.Tensor] = None):
     """Keep K of the T rows of `tensors`: the first `first`, the last `last` and the heaviest between, in order.  Returns (idx [K]
-    int32, the kept rows' weights, the cut-down tensors, the kept rows' pos or None)."""
+    int32, the kept rows' weights, the cut-down tensors, the kept rows' pos or None).  outs: where to, of K rows each, nothing that is read
+    (a cache cannot be cut down in place)."""
     return (_host or host()).cache_evict(weights, K, first, last, tensors, pos, outs, ws)
 
 

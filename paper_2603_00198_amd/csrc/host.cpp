@@ -524,6 +524,13 @@ struct On {
     const On &with(const Tensor *t) const { return t ? with(*t) : *this; }
 };
 
+// Whether the first bytes of two contiguous tensors share memory.
+bool share(const Tensor &a, size_t na, const Tensor &b, size_t nb) {
+    const uintptr_t x = (uintptr_t)a.data_ptr(), y = (uintptr_t)b.data_ptr();
+    return na && nb && x < y + nb && y < x + na;
+}
+bool share(const Tensor &a, const Tensor &b) { return share(a, a.nbytes(), b, b.nbytes()); }
+
 // Elements between the rows of a [rows, H, d] tensor whose rows are contiguous (a column range of a projection is fine).
 int64_t row_pitch(const Tensor &t, const char *what) {
     if (!t.is_cuda()) fail("tensors must live on the GPU");
@@ -631,6 +638,8 @@ struct Weights {
             if (t && (t->dim() != 1 || t->size(0) < T || !is_f32(*t))) fail(std::string(what) + ": weights must be fp32 [T]");
         on.with(in);
         if (want) on.with(out);
+        if (in && in->data_ptr() != out.data_ptr() && share(*in, 4 * (size_t)T, out, 4 * (size_t)T))
+            fail(std::string(what) + ": weights_out may be weights, but not a part of them moved on");
     }
     float *p() { return out.defined() ? f32(&out) : nullptr; }
     PyObject *py() { return out.defined() ? wrap(std::move(out)) : none(); }
@@ -709,6 +718,13 @@ PyObject *cache_evict(Args a) {  // weights, K, first, last, tensors, pos, outs,
         on.with(t).with(dst[i]);
         items[i] = {t.data_ptr(), dst[i].data_ptr(), sz.row() * (int64_t)t.element_size()};
     }
+    // rows are read and written in any order: what is given as an output is nothing that is read, and no other output
+    if (a[6] != Py_None)
+        for (int i = 0; i < n; ++i) {
+            bool apart = !share(dst[i], w) && !(pos && share(dst[i], *pos));
+            for (int j = 0; j < n; ++j) apart = apart && !share(dst[i], dev(list[j])) && (j == i || !share(dst[i], dst[j]));
+            if (!apart) fail("cache_evict: output " + std::to_string(i) + " overlaps an input or another output");
+        }
     Tensor idx = empty({K}, at::kInt, w), kept = empty({K}, at::kFloat, w), pos_out;
     if (pos) pos_out = empty({K}, at::kInt, w);
     Workspace ws(a[7], a[7] == Py_None ? strd_cache_evict_workspace(T, K, first, last) : 0, w, on.st);

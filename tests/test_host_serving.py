@@ -267,3 +267,28 @@ def test_more_kv_heads_than_32_bit_offsets_reach_are_refused():
         for i in pitches:
             args[i] = 65535 * 32
         assert getattr(L, name)(*args) == EHIP, name
+
+
+@pytest.mark.gpu
+def test_binding_refuses_outputs_on_top_of_what_is_read():
+    """A cut in place would read rows that are written already; weights that step over themselves would be added twice."""
+    d = "cuda"
+    w, pos = torch.rand(40, device=d), torch.arange(40, dtype=torch.int32, device=d)
+    x, y = torch.randn(40, 4, device=d), torch.randn(40, 4, device=d)
+    both = torch.empty(30, 4, device=d)
+    q, k = torch.zeros(4, 64, device=d), torch.zeros(36, 2, 64, device=d)
+    c = strd.Kv4Cache.empty(36, 2, 64)
+    bad = [lambda: strd.cache_evict(w, 10, 2, 2, [x], outs=[x[:10]]),
+           lambda: strd.cache_evict(w, 10, 2, 2, [x, y], outs=[y[30:], x[30:]]),
+           lambda: strd.cache_evict(w, 10, 2, 2, [x, y], outs=[both[:10], both[5:15]]),
+           lambda: strd.cache_evict(w, 8, 2, 2, [x[:, 0].contiguous()], outs=[w[8:16]]),
+           lambda: strd.cache_evict(w, 8, 2, 2, [pos.clone()], pos=pos, outs=[pos[32:]]),
+           lambda: strd.attn_decode_step_weights(q, k, k, weights=w, weights_out=w[4:]),
+           lambda: strd.attn_decode_step_kv4(q, c, 36, weights=w[4:], weights_out=w)]
+    for i, call in enumerate(bad):
+        with pytest.raises(strd.StrdError):
+            call()
+            print("case", i, "was taken")
+    idx, _, outs, _ = strd.cache_evict(w, 10, 2, 2, [x, y], outs=[both[:10], both[10:20]])
+    assert torch.equal(both[:10], x[idx.long()]) and torch.equal(both[10:20], y[idx.long()])
+    strd.attn_decode_step_weights(q, k[:4], k[:4], weights=w, weights_out=w[4:])   # the first 4 only are read
