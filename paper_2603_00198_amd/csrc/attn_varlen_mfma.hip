@@ -367,9 +367,9 @@ __global__ __launch_bounds__((G * NW + NC) * kWave) __attribute__((amdgpu_waves_
                 if (edge) hide_scores(-INFINITY);
                 if constexpr (CAP || BIAS)
                     lds_issue_tr8<0, 16 * kRowB, 32, 16 * kRowB + 32, 64, 16 * kRowB + 64, 96, 16 * kRowB + 96>(vp, vr8[0]);
-                // The probabilities, against the reference as it is (of a row that has seen no key yet: 0).  The row sum is taken of
-                // them as they enter the second product, i.e. rounded to bf16 (numerator and denominator then carry the same
-                // rounding), two at a time.
+                // The probabilities, against the reference as it is (of a row that has seen no key yet: 0), rounded to bf16 for the second product as in
+                // attn_mfma.hip: in two parts they would take half of all products again, 235 us of 8320 tokens' 590 at the rate of a large one.  The row
+                // sum is taken of them as they enter the product (numerator and denominator then carry the same rounding), two at a time.
                 bf16x8 pf[2];
                 float ps[2];
                 auto probabilities = [&](const float (&less)[2]) __attribute__((always_inline)) {
@@ -598,7 +598,8 @@ int attn_varlen_mfma(const void *q, const void *k, const void *v, void *o, int H
     pr.scale2 = mod.scale * kLog2e;
     pr.kappa = 2.f * kLog2e * mod.scale * mod.inv_cap;
     pr.c2 = mod.cap * kLog2e, pr.c2_twice = -2.f * pr.c2;
-    // tanh(y) / y up to y = 0.25 and 0.5, of least relative error (4.0e-7, 5.5e-7); y = ky raw goes into the coefficients.  Where those of the
+    // tanh(y) / y up to y = 0.25 and 0.5, of least relative error (4.0e-7, 5.5e-7: 5e-6 and 1.4e-5 of a score under a cap of 50, where the probability's
+    // rounding to bf16 is 4e-3); y = ky raw goes into the coefficients.  Where those of the
     // higher powers leave fp32's range (a cap far above every score) the polynomials end before they count, where they are too large (a cap far
     // below) the exponential form, whose absolute error is a few steps of the cap, takes every score.
     const double near_y[3] = {0.99999960434, -0.33321908205, 0.12841613181}, half_y[4] = {0.999999452, -0.333263082, 0.131902465, -0.0444017053};
