@@ -262,7 +262,7 @@ int strd_compact_varlen(const strd_compact_item *items, int n_items, const int32
  *   S_in  [dev] [H, P, n] fp32 or NULL (zero state)
  *   y     [dev] [T, H, P]        S_out [dev] [H, P, n] fp32 or NULL
  * The bf16 matrix-core kernels add D x_t inside the token product (D joins the bf16 weight of
- * token t on itself), i.e. that term carries a relative rounding error of up to 2^-9, like every
+ * token t on itself), i.e. that term carries a relative rounding error of up to 2^-8, like every
  * other term of the sum and like the bf16 output itself.
  * Long bf16 sequences are cut into segments: there the part of an output that the state carries is rounded to bf16
  * before it is added (not where four heads of a group and P = 64 go together, from 64 heads on), and the first outputs of

@@ -13,7 +13,7 @@
 //  * Values: A = the codes of V with the cache's rows as the contraction index, B = p * s -- p comes from the lane that has it with the
 //    multiplication itself -- for every (head, group), as two bf16 numbers, its upper 8 bits and the rest, in two products: what is left out is
 //    2^-16 of a weight, where bf16 alone left 2^-8 (a step over 131627 rows 59.4 -> 59.6 us, over 8491 plain ones 11.9 -> 12.0, with 8 heads to a kv head
-//    60.3 -> 64.7).  A lane collects 8 rows' codes and regroups their halves.  What the 24 too many and z add does not depend on the channel: each lane sums
+//    71.6 -> 73.2).  A lane collects 8 rows' codes and regroups their halves.  What the 24 too many and z add does not depend on the channel: each lane sums
 //    p z - 24 (both parts of p s) in fp32.  Rows (channels) of the product and columns of another group belong to nobody.
 //  * A plain cache goes the same way without groups: columns are heads, values are regrouped halves.  The lower part is 2^-24 of the weight
 //    at least there: where it is 0 an infinite value would become NaN.

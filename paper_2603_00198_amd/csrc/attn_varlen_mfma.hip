@@ -13,8 +13,8 @@
 //    added at the end, row by row.  And a row's softmax reference moves by the row's own scores alone, never because of a neighbour in its wave: its
 //    result has the same bits whatever the rows that it does not see hold.
 // Bound by the matrix products and the vector instructions of a SIMD, which overlap only in part (attn_mfma.hip), and for short
-// batches by the start and end of a workgroup.  us: 8320 tokens, 32 / 8 heads of 128: 490 (1.16 PFLOP/s), biased 519, cap 50 580 to 590, both 643;
-// 2176 tokens, biased 63; six sequences of 3493 tokens, 28 / 4 heads of 64, prefix 41.  A cap of 15 at scores of deviation 1 629, one that
+// batches by the start and end of a workgroup.  us: 8320 tokens, 32 / 8 heads of 128: 498 (1.14 PFLOP/s), biased 535, cap 50 571 to 600, both 627;
+// 2176 tokens, biased 64; six sequences of 3493 tokens, 28 / 4 heads of 64, prefix 41.  A cap of 15 at scores of deviation 1 629, one that
 // every score is beyond 790; where some rows of a wave's blocks are beyond half of it and some not, both forms are computed: twice the time.
 #include "attn_varlen.h"
 
