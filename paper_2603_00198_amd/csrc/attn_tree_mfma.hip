@@ -316,7 +316,8 @@ __global__ __launch_bounds__((NW + NC) * kWave) __attribute__((amdgpu_waves_per_
                 if constexpr (CAP) weights([&](int, float x) { return x; });
                 // (a reference far from zero has no place in the instruction that gives an exponent: what is rounded off it there may be a power of
                 // two that a sum does not hold)
-                else if (__builtin_expect(far_ref, 0)) weights([&](int qt, float x) { return (x - ref[qt]) * scale2; });
+                // (and a row of the wave that has not seen a key yet has none to take off: -infinity less itself is NaN)
+                else if (__builtin_expect(far_ref, 0)) weights([&](int qt, float x) { return (x - (ref[qt] == -INFINITY ? 0.f : ref[qt])) * scale2; });
                 else weights([&](int qt, float x) { return fmaf(x, scale2, BIAS ? ref[qt] == -INFINITY ? 0.f : -ref[qt] * scale2 : less[qt]); });  // (registers)
             };
             all_weights();
