@@ -210,11 +210,13 @@ __global__ __launch_bounds__((NW + NC) * kWave) __attribute__((amdgpu_waves_per_
     f32x4 oacc[DT][2];
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) oacc[dt][0] = oacc[dt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-    // per row: the reference in units of log2 e, -infinity before the first key, and what is added to an exponent for it; l_run: this lane group's
-    // share of the sum
+    // per row: the reference, -infinity before the first key, and what is added to an exponent for it (with a cap to a score; 0 where it is far from zero);
+    // l_run: this lane group's share of the sum
     float ref[2] = {-INFINITY, -INFINITY}, less[2] = {0.f, 0.f}, l_run[2] = {0.f, 0.f};
     const float scale2 = CAP ? 1.f : pr.scale2;  // scores' units -> log2 (with a cap the scores are in them)
     bool far_ref = false;  // uniform: some row's reference is far from zero
+    // (or its capped scores may be: with a bias of their size a reference may be anywhere)
+    auto is_far = [&](float r) { return r > -INFINITY && ((CAP && pr.c2 > kFar) || fabsf(r * scale2) > kFar); };
     const bool live = 32 * (NW * rb + w) < R;
 
     constexpr int kRowB = TileT::kPitch * 2;
@@ -313,11 +315,11 @@ __global__ __launch_bounds__((NW + NC) * kWave) __attribute__((amdgpu_waves_per_
                 }
             };
             auto all_weights = [&]() __attribute__((always_inline)) {
-                if constexpr (CAP) weights([&](int, float x) { return x; });
-                // (a reference far from zero has no place in the instruction that gives an exponent: what is rounded off it there may be a power of
-                // two that a sum does not hold)
-                // (and a row of the wave that has not seen a key yet has none to take off: -infinity less itself is NaN)
-                else if (__builtin_expect(far_ref, 0)) weights([&](int qt, float x) { return (x - (ref[qt] == -INFINITY ? 0.f : ref[qt])) * scale2; });
+                // A reference far from zero has no place in the instruction that gives an exponent or, with a cap, a score: what is rounded off it there
+                // may be a power of two that a sum does not hold.  It is taken off the scores themselves.  (A row of the wave that has not seen a key yet
+                // has none to take off: -infinity less itself is NaN.)
+                if (__builtin_expect(far_ref, 0)) weights([&](int qt, float x) { return (x - ((CAP ? is_far(ref[qt]) : ref[qt] > -INFINITY) ? ref[qt] : 0.f)) * scale2; });
+                else if constexpr (CAP) weights([&](int, float x) { return x; });
                 else weights([&](int qt, float x) { return fmaf(x, scale2, BIAS ? ref[qt] == -INFINITY ? 0.f : -ref[qt] * scale2 : less[qt]); });  // (registers)
             };
             all_weights();
@@ -336,7 +338,7 @@ __global__ __launch_bounds__((NW + NC) * kWave) __attribute__((amdgpu_waves_per_
 #pragma unroll
                     for (int dt = 0; dt < DT; ++dt) oacc[dt][qt] *= corr;
                     ref[qt] = now;
-                    const float add = now == -INFINITY ? 0.f : -now * scale2;
+                    const float add = now == -INFINITY || (CAP && is_far(now)) ? 0.f : -now * scale2;
                     if constexpr (CAP) {
 #pragma unroll
                         for (int j = 0; j < 2; ++j)
@@ -345,7 +347,7 @@ __global__ __launch_bounds__((NW + NC) * kWave) __attribute__((amdgpu_waves_per_
                     }
                     less[qt] = add;
                 }
-                far_ref = !CAP && __any(fmaxf(fabsf(less[0]), fabsf(less[1])) > kFar);
+                far_ref = __any(is_far(ref[0]) || is_far(ref[1]));
                 all_weights();
             }
             l_run[0] += ps[0];

@@ -39,3 +39,32 @@ def test_tree_nodes_that_see_nothing_beside_scores_far_from_zero(size, cap, slop
     mag = np.repeat((np.abs(vv[0:m - 1:2]) + np.abs(vv[1:m:2])) / 2, Hq // Hkv, axis=1)
     # weights of 1 each: a sum of two, and a division
     base._within(o[1::2], want, 4 * U32 * mag + HALF[dtype] * np.abs(want), "o")
+
+
+@pytest.mark.parametrize("dtype,d,Hq,Hkv,m", [(BF16, 64, 4, 1, 8), (BF16, 128, 8, 2, 16), (BF16, 96, 4, 1, 32), (BF16, 64, 8, 1, 40), (BF16, 128, 8, 1, 40), (F32, 64, 4, 2, 11)])
+@pytest.mark.parametrize("cap", [0.0, 20.0, 1e9])
+@pytest.mark.parametrize("T", [100, 3000])
+def test_tree_equal_scores_far_from_zero(T, cap, dtype, d, Hq, Hkv, m):
+    """Rows of the cache at one position that is 2^24 - 1 from the nodes', of one key: whatever the slope, from none to 64, and whatever block or split they are
+    in, they weigh the same, a sum of T of them and a division away from their mean.  Every other node sees itself, at its own position: where there is a slope
+    that is all it sees."""
+    base._say("tree equal scores", T, cap, dtype, d, Hq, Hkv, m)
+    g = torch.Generator().manual_seed(T + m)
+    far = 2.0 if cap < 1e9 else 3e3   # (with the high cap scores of 1e6 and more)
+    q = base._rand(g, m, Hq, d, dtype=dtype, size=far)
+    k = base._rand(g, 1, Hkv, d, dtype=dtype, size=far).expand(T + m, Hkv, d).contiguous()
+    v = base._rand(g, T + m, Hkv, d, dtype=dtype)
+    sl = torch.tensor([0.0, 1.0, 8.0, 64.0], dtype=F32).repeat(Hq // 4)
+    ps = torch.cat([torch.zeros(T), torch.full((m,), 2.0 ** 24 - 1)]).to(torch.int32)
+    mask = torch.tensor([1 << i if i % 2 else 0 for i in range(m)], dtype=torch.int64)
+    o = strd.attn_tree_step(*(base._dev(t) for t in (q, k[:T], v[:T], k[T:], v[T:], mask)), cap=cap, slopes=base._dev(sl), pos=base._dev(ps))
+    vv, rep = np64(v), Hq // Hkv
+    want, mag = np.zeros((m, Hq, d)), np.zeros((m, Hq, d))
+    for i in range(m):
+        for h in range(Hq):
+            seen = vv[:T, h // rep]
+            if i % 2:
+                seen = vv[T + i:T + i + 1, h // rep] if sl[h] else np.concatenate([seen, vv[T + i:T + i + 1, h // rep]])
+            want[i, h], mag[i, h] = seen.mean(0), np.abs(seen).mean(0)
+    # (a weight is rounded to bf16 before the product; it is a power of two or 1 here, or all of a row's are the same number)
+    base._within(o, want, (T + m) * U32 * mag + (2 * 2.0 ** -8 * mag if dtype == BF16 else 0) + HALF[dtype] * np.abs(want) + 1e-30, "o")
