@@ -504,7 +504,7 @@ int strd_cache_evict(const float *w, int T, int K, int first, int last, const st
  *   addresses are whole multiples of that, else one).
  * conv1d_silu_step -- the same for one token each of `batch` sequences, and the softplus of dt with it: row [dev] [batch] of pitch
  *   ld >= Ct + H, dt_out[e, h] = log(1 + exp(row[e, Ct + h] + dt_bias[h])) fp32 (H = 0: none; dt_bias [H] fp32 or NULL).  Both windows are
- *   needed if W > 1.  batch <= 65535.
+ *   needed if W > 1 (W = 1: nslots still bounds the slots).  batch <= 65535.
  *
  * ssd_prefill_varlen -- strd_ssd_prefill for a packed batch: x, dt, B, C, y with the rows of all sequences; S_in, S_out [dev]
  *   [nslots, H, P, n] fp32.  Workspace [dev], 16-byte aligned: strd_ssd_prefill_varlen_workspace bytes for the same descriptors

@@ -437,11 +437,12 @@ def conv1d_silu_varlen(xbc: torch.Tensor, w: torch.Tensor, b: Optional[torch.Ten
     return (_host or host()).conv1d_silu_varlen(xbc, w, b, Cx, Cb, seqs, window, window_out, slots, fresh)
 
 
-def conv1d_silu_step(row: torch.Tensor, w: torch.Tensor, b: Optional[torch.Tensor], Cx: int, Cb: int, window: torch.Tensor,
-                     window_out: Optional[torch.Tensor] = None, slots: Optional[torch.Tensor] = None, H: int = 0,
+def conv1d_silu_step(row: torch.Tensor, w: torch.Tensor, b: Optional[torch.Tensor], Cx: int, Cb: int,
+                     window: Optional[torch.Tensor] = None, window_out: Optional[torch.Tensor] = None, slots: Optional[torch.Tensor] = None, H: int = 0,
                      dt_bias: Optional[torch.Tensor] = None):
     """The same for one token each of many sequences: row [batch, >=Cx+2Cb+H], slots [batch] int32 on the GPU (None: entry e has slot e; outside
-    the pool, or one that an earlier entry has: the entry is left out, its outputs are zeros).  Returns x, B, C and dt [batch,H] fp32 =
+    the pool, or one that an earlier entry has: the entry is left out, its outputs are zeros).  A filter of one tap carries nothing: window may
+    be None, and any slot from 0 on will do.  Returns x, B, C and dt [batch,H] fp32 =
     softplus of the H columns behind C (+ dt_bias), or None if H is 0."""
     return (_host or host()).conv1d_silu_step(row, w, b, Cx, Cb, window, window_out, slots, H, dt_bias)
 

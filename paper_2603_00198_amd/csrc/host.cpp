@@ -858,7 +858,8 @@ PyObject *conv1d_silu_step(Args a) {  // row, w, b, Cx, Cb, window, window_out, 
     on.with(w).with(b).with(bias);
     const strd_dtype io = io_of(in);
     const int W = size(w, 1), batch = size(in, 0);
-    const Pool pool(a[5], a[6], {W - 1, Ct}, in.scalar_type(), on, what);
+    Pool pool(a[5], a[6], {W - 1, Ct}, in.scalar_type(), on, what);
+    if (W == 1 && !pool.out) pool.nslots = INT_MAX;  // one tap carries nothing: any slot from 0 on will do
     pool.apart(&in, what).apart(&w, what).apart(b, what).apart(bias, what);
     const Tensor *const slots = entries(a[7], batch, on, what);
     pool.apart(slots, what);

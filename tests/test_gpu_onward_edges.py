@@ -68,3 +68,28 @@ def test_tree_equal_scores_far_from_zero(T, cap, dtype, d, Hq, Hkv, m):
             want[i, h], mag[i, h] = seen.mean(0), np.abs(seen).mean(0)
     # (a weight is rounded to bf16 before the product; it is a power of two or 1 here, or all of a row's are the same number)
     base._within(o, want, (T + m) * U32 * mag + (2 * 2.0 ** -8 * mag if dtype == BF16 else 0) + HALF[dtype] * np.abs(want) + 1e-30, "o")
+
+
+# ------------------------------------------------------------------ single tokens of a filter of one tap
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("listed", [False, True])
+def test_conv_step_of_one_tap_needs_no_window(listed, dtype):
+    """Nothing is carried, so there is no pool whose size a slot could be past; a batch may still be padded."""
+    base._say("conv step one tap", listed, dtype)
+    g = torch.Generator().manual_seed(3)
+    batch, Cx, Cb, H = 5, 32, 8, 3
+    row, w, b, bias = (base._rand(g, *s, dtype=t) for s, t in (((batch, 48 + H), dtype), ((48, 1), dtype), ((48,), dtype), ((H,), F32)))
+    slots = torch.tensor([900, -1, 0, 900, 7], dtype=torch.int32) if listed else None
+    args = [base._dev(t) for t in (row, w, b)]
+    live = [0, 2, 4] if listed else list(range(batch))
+    for pool in (None, torch.zeros(1000, 0, 48, dtype=dtype, device=DEV)):
+        x, B, C, dt = strd.conv1d_silu_step(*args, Cx, Cb, pool, slots=base._dev(slots), H=H, dt_bias=base._dev(bias))
+        got, want, mag = torch.cat([x, B, C], 1), np64(w)[:, 0] * np64(row)[:, :48] + np64(b), np.abs(np64(w)[:, 0] * np64(row)[:, :48]) + np.abs(np64(b))
+        o = plain.silu(want)
+        base._within(got[live], o[live], base._conv_bound(o, want, mag, 1, dtype)[live], "o")
+        raw = np64(row)[:, 48:] + np64(bias)
+        steps = np.logaddexp(0.0, raw)
+        size = np.abs(np64(row)[:, 48:]) + np.abs(np64(bias))
+        base._within(dt[live], steps[live], (steps * (3 * size + 16) * 2 * U32)[live], "dt")
+        rest = [i for i in range(batch) if i not in live]
+        assert (got[rest] == 0).all() and (dt[rest] == 0).all()
