@@ -93,3 +93,76 @@ def test_conv_step_of_one_tap_needs_no_window(listed, dtype):
         base._within(dt[live], steps[live], (steps * (3 * size + 16) * 2 * U32)[live], "dt")
         rest = [i for i in range(batch) if i not in live]
         assert (got[rest] == 0).all() and (dt[rest] == 0).all()
+
+
+# ------------------------------------------------------------------ packed scans: tokens that reset a head
+def _fine_scan(x, dt, A, B, C, D, S):
+    """One sequence in 64 bits (x [T, H, P], B, C [T, H, n]) -> y, S and bounds of fp32 arithmetic without a factor of all T: a partial sum is rounded where
+    it is made and decays with what it holds.  With term_j what token j leaves in the state now and l_j the exponent (base 2) of its decay,
+        n = sum_j (tokens since j + 1) |term_j|,   l = sum_j |l_j| |term_j|,   m = sum_j |term_j|.
+    Returns y and S, their fp32 error bounds, and the sums of absolute values under both."""
+    T, H, P = x.shape
+    S, m = S.copy(), np.abs(S)
+    n, l = m.copy(), np.zeros_like(m)
+    y, ey, my = np.zeros(x.shape), np.zeros(x.shape), np.zeros(x.shape)
+    width = B.shape[2]
+    for t in range(T):
+        d = dt[t] * A
+        a = np.exp(d)[:, None, None]
+        add = (dt[t][:, None] * x[t])[:, :, None] * B[t][:, None, :]
+        # (what is left of l is a power of two far from 1: nothing beyond 2^-200)
+        l = a * (l + np.minimum(np.abs(d) / np.log(2), 200.0)[:, None, None] * m)
+        S, m = a * S + add, a * m + np.abs(add)
+        n = a * n + m
+        c = C[t][:, :, None]
+        y[t] = (S @ c)[..., 0] + (0 if D is None else D[:, None] * x[t])
+        skip = 0 if D is None else np.abs(D[:, None] * x[t])
+        my[t] = (m @ np.abs(c))[..., 0] + skip
+        # additions and products of the state; up to 32 roundings of an exponent, in sums and products; 64 + n of the product with c and of factors
+        ey[t] = (((2 * n + 32 * l) @ np.abs(c))[..., 0] + (128 + width) * my[t]) * 2 * U32
+    return y, S, ey, (2 * n + 32 * l + (128 + width) * m) * 2 * U32, my, m
+
+
+def _heads(H, G, some):
+    return [h * G // H for h in some]
+
+
+def _check_fine(seqs, x, dt, A, B, C, D, pool, slots, fresh, got, after, roundings, some=None):
+    """Heads `some` (None: all) of a packed scan: states as fp32 sums -- two pieces of bf16 leave out 2^-16 of a term at most --, outputs with `roundings` of
+    what they sum to bf16 and their own."""
+    H, G = x.shape[1], B.shape[1]
+    some = list(range(H)) if some is None else some
+    gs = _heads(H, G, some)
+    X, DT, AA, BB, CC = np64(x[:, some]), np64(dt[:, some]), np64(A[some]), np64(B[:, gs]), np64(C[:, gs])
+    DD, r, half = None if D is None else np64(D[some]), 0, HALF[x.dtype]
+    for i, s in enumerate(seqs):
+        at = slice(r, r + s[0] + s[1])
+        r = at.stop
+        S0 = np64(pool[slots[i], some]) if pool is not None and not (fresh is not None and fresh[i]) else np.zeros((len(some), x.shape[2], B.shape[2]))
+        y, S, ey, eS, my, m = _fine_scan(X[at], DT[at], AA, BB[at], CC[at], DD, S0)
+        inner = ey + roundings * 2.0 ** -8 * (1 + 2.0 ** -7) * my
+        base._within(got[at][:, some], y, inner + half * (np.abs(y) + inner) + 1e-37, "y of sequence %d" % i)
+        if after is not None:
+            base._within(after[slots[i], some], S, eS + (2.0 ** -16 * m if x.dtype == BF16 else 0) + 1e-37, "state of sequence %d" % i)
+
+
+RESETS = [(BF16, 64, 4, 64, 64), (BF16, 32, 2, 128, 64), (BF16, 8, 2, 128, 64), (F32, 8, 2, 64, 64), (BF16, 6, 6, 24, 40)]
+
+
+@pytest.mark.parametrize("dtype,H,G,n,P", RESETS)
+@pytest.mark.parametrize("size", [300.0, 1e4, 1e6, 1e9])
+def test_scan_varlen_goes_on_behind_tokens_that_reset_a_head(size, dtype, H, G, n, P):
+    """A token in thirty decays its head by e^-size and brings nothing itself: what comes behind it in the same few tokens keeps its weights, which are not
+    differences of numbers that large."""
+    base._say("scan resets", size, dtype, H, G, n, P)
+    seqs = [(700, 5, 0), (290, 10, 0)] + [(i % 7, i % 3 + 1, 0) for i in range(16)]
+    rows = sum(s[0] + s[1] for s in seqs)
+    x, dt, A, B, C, D = base._scan_case(rows, H, P, G, n, dtype, seed=6)
+    dt *= 0.02
+    reset = torch.rand((rows, H), generator=torch.Generator().manual_seed(1)) < 1 / 30
+    dt[reset] = (-size / A).expand(rows, H)[reset]
+    x[reset] = 0
+    pool = base._rand(torch.Generator().manual_seed(2), len(seqs), H, P, n)
+    state = base._dev(pool)
+    y = strd.ssd_prefill_varlen(*(base._dev(t) for t in (x, dt, A, B, C)), seqs, base._dev(D), state=state)
+    _check_fine(seqs, x, dt, A, B, C, D, pool, list(range(len(seqs))), None, y, state, 0 if dtype == F32 else 2, some=list(range(0, H, max(1, H // 8))))
