@@ -510,7 +510,8 @@ int strd_cache_evict(const float *w, int T, int K, int first, int last, const st
  *   [nslots, H, P, n] fp32.  Workspace [dev], 16-byte aligned: strd_ssd_prefill_varlen_workspace bytes for the same descriptors
  *   (STRD_EWORKSPACE).  H % G == 0; n <= 1024, H * P * n <= 2^30 (else STRD_EUNSUPPORTED).  bf16 heads of P = 64 in groups of whole
  *   fours with n = 64 or 128 run on the bf16 matrix cores: x, B, C, y and both pools 16-byte aligned (else STRD_EINVAL), two roundings to
- *   bf16 in an output, none in a state; sums of more than 2^79 in a state may leave fp32.  Small batches of them run in fp32, as does
+ *   bf16 in an output (a third of what earlier tokens left, where each of heads 4 i to 4 i + 3 decays by 2^-12 or more in every 32 tokens of a stretch),
+ *   none in a state; sums of more than 2^79 in a state may leave fp32.  Small batches of them run in fp32, as does
  *   every other shape and type, those at any alignment.  Final states are fp32 sums either way.  Where sequences are cut follows from
  *   the whole batch, and with it the last bits of a result.  Values that are not finite stay in their own sequence; there they show in
  *   every later output of their channel (dt: of their head) and, as tokens are weighed in blocks, up to 63 tokens earlier.

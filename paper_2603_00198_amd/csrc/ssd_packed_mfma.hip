@@ -8,7 +8,8 @@
 //    are completed later reads and rounds most outputs twice where heads remember for long.)  The same sums are the final states, fp32 numbers.
 //  * w x in pieces.  S += b^T (w x) has exact bf16 numbers b and x, but w = dt 2^(decay to the end) has 24 bits.  w x goes into the product as bf16 numbers, each
 //    the rest of those before it: three for the states, two in the walk, whose outputs then pass two roundings to bf16 on any way (of a weight or of
-//    the state, and their own), one where heads forget within a step, so that little passes through the state at all.
+//    the state, and their own).  One, and three roundings of what passes through the state, where all four heads forget within every step of the segment:
+//    there that is a few tokens' part of an output.
 //  * States in units.  Where heads remember a state decays by its unit, which the weights of tokens and the factors of outputs take in; it is multiplied only
 //    where the unit has gone 2^48 away: 64 multiplications of a wave and step less (33280 tokens of slow heads 353 -> 293 us; where heads forget within a
 //    step it would be multiplied as often, and not between the products: 277 -> 334).
@@ -31,7 +32,7 @@ namespace {
 constexpr float kGone = -150.f;     // log2 of a decay that leaves nothing in fp32
 constexpr float kReset = -200.f;    // ... nor after a unit below has been taken off it
 constexpr float kApart = 48.f;      // log2 of how far a state's unit may be from 1
-constexpr float kForgets = -12.f;  // log2 of the decay over a step from which on w x is taken in one piece
+constexpr float kForgets = -12.f;  // log2 of the decay over every step of a segment from which on w x is taken in one piece
 
 struct PackArgs {
     const bf16_t *x;
@@ -75,8 +76,8 @@ struct PackArgs {
 
 template <int NS>
 struct LdsP : LdsQ<NS> {
-    float sums[kThreads / 64][kHeads];  // of the steps' decays, per wave
-    float anew[3][kHeads];              // what a state is multiplied by in a step for its new unit, or 1
+    int remembers[kThreads / 64];  // per wave, whether it has seen a step beyond which a head remembers
+    float anew[3][kHeads];         // what a state is multiplied by in a step for its new unit, or 1
 };
 static_assert(sizeof(LdsP<128>) <= 160 * 1024, "one workgroup must fit the 160 KB of LDS of a CU");
 
@@ -460,27 +461,19 @@ __global__ __launch_bounds__(kThreads) void ssd_packed_kernel(PackArgs a) {
     const float *s_src = seg ? a.init + (size_t)(a.first[s] + seg) * state : a.S_in && !(a.fresh >> s & 1) ? a.S_in + (size_t)a.slot[s] * state : nullptr;
     uint32_t *lost = a.lost + (size_t)useg * a.H * 2;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    // Whether some head remembers beyond a step: its mean decay over one.
-    float part[kHeads] = {};
-    for (int i = (int)threadIdx.x; i < nloc; i += kThreads) {
+    // Whether some head remembers beyond some step (other than the last, whose state nothing reads: resets on the way do not speak for the rest).
+    bool mine = false;
+    for (int i = (int)threadIdx.x; i + 1 < nloc; i += kThreads) {
         const f32x4 d = *reinterpret_cast<const f32x4 *>(a.decay + (size_t)(a.step0[s] + seg * a.steps[s] + i) * a.H + h0);
 #pragma unroll
-        for (int k = 0; k < kHeads; ++k) part[k] += d[k];
+        for (int k = 0; k < kHeads; ++k) mine |= !(d[k] <= kForgets);
     }
-#pragma unroll
-    for (int k = 0; k < kHeads; ++k) {
-        const float sum = wave_inclusive_scan_f32(part[k]);
-        if ((threadIdx.x & 63) == 63) lds.sums[wave][k] = sum;
-    }
+    mine = __any(mine);
+    if ((threadIdx.x & 63) == 0) lds.remembers[wave] = mine;
     lds_barrier();
     bool more = false;
 #pragma unroll
-    for (int k = 0; k < kHeads; ++k) {
-        float sum = 0.f;
-#pragma unroll
-        for (int w = 0; w < kThreads / 64; ++w) sum += lds.sums[w][k];
-        more |= !(sum <= kForgets * (float)nloc);
-    }
+    for (int w = 0; w < kThreads / 64; ++w) more |= lds.remembers[w] != 0;
     more = __builtin_amdgcn_readfirstlane(more);
     // Wave i runs on SIMD i % 4: every SIMD has two compute waves and one of the others.
     if (wave < 8 && more)

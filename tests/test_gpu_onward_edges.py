@@ -166,3 +166,23 @@ def test_scan_varlen_goes_on_behind_tokens_that_reset_a_head(size, dtype, H, G, 
     state = base._dev(pool)
     y = strd.ssd_prefill_varlen(*(base._dev(t) for t in (x, dt, A, B, C)), seqs, base._dev(D), state=state)
     _check_fine(seqs, x, dt, A, B, C, D, pool, list(range(len(seqs))), None, y, state, 0 if dtype == F32 else 2, some=list(range(0, H, max(1, H // 8))))
+
+
+@pytest.mark.parametrize("H,G,n", [(64, 4, 64), (32, 2, 128)])
+def test_scan_varlen_a_reset_does_not_cost_the_steps_that_remember_a_rounding(H, G, n):
+    """A reset, one token that writes and many that read it, again and again, with next to nothing forgotten in between: an output is one term, which passes two
+    roundings to bf16, of its weight or of the state and its own, however strong the resets are on average.  Terms are a little above 1, where half a step is
+    largest, so that three roundings show."""
+    base._say("scan resets between steps that remember", H, G, n)
+    P, T = 64, 1920
+    g = torch.Generator().manual_seed(5)
+    x, dt = torch.zeros(T, H, P, dtype=BF16), torch.full((T, H), 1e-3)
+    x[1::96] = (1.0 + torch.randint(8, 13, (T // 96, H, P), generator=g) / 128).to(BF16)
+    dt[1::96] = 1.0 + 0.05 * torch.rand((T // 96, H), generator=g)
+    dt[0::96] = 1e4
+    A = -0.6 - 0.1 * torch.rand(H, generator=g)
+    B, C = torch.zeros(T, G, n, dtype=BF16), torch.zeros(T, G, n, dtype=BF16)
+    B[..., 3] = C[..., 3] = 1
+    seqs = [(T, 0, 0)]
+    y = strd.ssd_prefill_varlen(*(base._dev(t) for t in (x, dt, A, B, C)), seqs)
+    _check_fine(seqs, x, dt, A, B, C, None, None, [0], None, y, None, 1)
