@@ -501,7 +501,7 @@ int strd_cache_evict(const float *w, int T, int K, int first, int last, const st
  * conv1d_silu_varlen -- strd_conv1d_silu for a packed batch: rows before a sequence's first are those of its window, oldest first.
  *   xbc [dev] rows of pitch ld >= Ct = Cx + 2 Cb elements; window_in, window_out [dev] [nslots, W - 1, Ct] of the io dtype; w, b, outputs as
  *   there.  1 <= W <= 4 (else STRD_EUNSUPPORTED); any Cx, Cb, ld and alignment (16 bytes of channels at a time where Cx, Cb, ld and all
- *   addresses are whole multiples of that, else one).
+ *   addresses are whole multiples of that, else one, and rows * Ct up to 2^34 then, else STRD_EUNSUPPORTED).
  * conv1d_silu_step -- the same for one token each of `batch` sequences, and the softplus of dt with it: row [dev] [batch] of pitch
  *   ld >= Ct + H, dt_out[e, h] = log(1 + exp(row[e, Ct + h] + dt_bias[h])) fp32 (H = 0: none; dt_bias [H] fp32 or NULL).  Both windows are
  *   needed if W > 1 (W = 1: nslots still bounds the slots).  batch <= 65535.
@@ -524,7 +524,7 @@ int strd_cache_evict(const float *w, int T, int K, int first, int last, const st
  *   q, k, q_out, k_out [dev] rows of Hq (Hkv) heads of d channels, of pitches ldq .. ldko in elements (>= a row's own); an output may be its
  *   input, pitch included, or share no element with q, k or the other output (else STRD_EINVAL).  Hq or Hkv may be 0 (pointers then unused).
  *   pos [dev] [rows] int32, any sign (after a compaction the rows' old positions); freq [dev] [rot / 2] fp32; angles are reduced in 64 bits,
- *   so far positions lose nothing.  2 <= rot <= d, rot even, amplitude finite; d <= 1024.
+ *   so far positions lose nothing.  2 <= rot <= d, rot even, amplitude finite; d <= 1024, rows <= 2^25 (else STRD_EUNSUPPORTED).
  * rope_frequencies -- freq for rot channels: base^(-2 i / rot), and for contexts longer than the `original` positions a model was trained on,
  *   `factor` times, the slow ones divided: with r = original * freq / (2 pi) turns in the trained length, those of r <= low are divided by factor,
  *   those of r >= high stay, between the two linear in r (low = high = infinity: all are divided; factor = 1: none).  freq_out [host] [rot / 2].
@@ -536,7 +536,7 @@ int strd_cache_evict(const float *w, int T, int K, int first, int last, const st
  *   visible (bits from m on are not looked at).  1 <= m <= 64, T >= 0 (0: no cache needed).  A node that sees nothing gets zeros; what a node does
  *   not see does not reach it, values that are not finite included.  Scores with cap and slopes as in attn_prefill_varlen above; pos [dev] [T + m]
  *   int32, the cache's rows first; NULL: a row's number, and for a node T + the number of other nodes that it sees (in a tree: its depth).
- *   d <= 256, Hq % Hkv == 0.  Workspace [dev], 16-byte aligned: strd_attn_tree_step_workspace bytes (STRD_EWORKSPACE).  Deterministic.
+ *   d <= 256, Hkv <= 65535, m * Hq <= 2^21 (else STRD_EUNSUPPORTED), Hq % Hkv == 0, T <= 2^30.  Workspace [dev], 16-byte aligned: strd_attn_tree_step_workspace bytes (STRD_EWORKSPACE).  Deterministic.
  * tree_mask -- mask of a tree: parent[i] in [-1, i) is node i's parent (-1: it hangs on the cache's last row); node i sees itself and its
  *   ancestors.  Host-only.  STRD_EINVAL for any other parent or m outside 1..64.
  *

@@ -735,7 +735,7 @@ int strd_rope(const void *q, int64_t ldq, void *q_out, int64_t ldqo, int Hq, con
     const int64_t wq = (int64_t)Hq * d, wk = (int64_t)Hkv * d;
     if ((Hq && (ldq < wq || ldqo < wq)) || (Hkv && (ldk < wk || ldko < wk))) return STRD_EINVAL;
     if (rows > 0 && (!pos || !freq || (Hq && (!q || !q_out)) || (Hkv && (!k || !k_out)))) return STRD_EINVAL;
-    if (d > 1024 || Hq > (1 << 20) || Hkv > (1 << 20) || ((long long)Hq + Hkv) * d > (1 << 28)) return STRD_EUNSUPPORTED;
+    if (d > 1024 || Hq > (1 << 20) || Hkv > (1 << 20) || ((long long)Hq + Hkv) * d > (1 << 28) || rows > (1 << 25)) return STRD_EUNSUPPORTED;
     if (rows == 0) return STRD_OK;
     const size_t es = io == STRD_F32 ? 4 : 2;
     const bool same_q = q == q_out && ldq == ldqo, same_k = k == k_out && ldk == ldko;
@@ -769,7 +769,7 @@ int strd_attn_tree_step(const void *q, const void *k_cache, const void *v_cache,
     if (T < 0 || T > kTreeMostRows || m < 1 || m > kTreeMost || Hq < 1 || Hkv < 1 || d < 1 || Hq % Hkv || !io_ok(io) || !(scale > 0.f) ||
         !cap_ok(cap) || !q || (T > 0 && (!k_cache || !v_cache)) || !k_new || !v_new || !mask || !o)
         return STRD_EINVAL;
-    if (d > 256 || Hkv > 65535 || Hq > (1 << 20)) return STRD_EUNSUPPORTED;
+    if (d > 256 || Hkv > 65535 || (long long)m * Hq > (1 << 21)) return STRD_EUNSUPPORTED;
     const size_t need = attn_tree_ws(T, m, Hq, Hkv, d, io);
     if (!ws || ws_bytes < need || !aligned16(ws)) return STRD_EWORKSPACE;
     cap = cap_in_range(cap);

@@ -190,7 +190,7 @@ int conv_varlen(const void *xbc, long long ld, const void *w, const void *b, con
     if (few) plan_carry(seqs, nseq, false, nslots, slots, fresh, kFewTok, always, tab, rows);
     const int tiles = tab.base[nseq];
     const long long units = ((long long)tiles * vecs + kThreads - 1) / kThreads;
-    if (units > 0x7FFFFFF0LL) return STRD_EUNSUPPORTED;
+    if (units > (1 << 24) - kXcd) return STRD_EUNSUPPORTED;  // threads of a launch have 32 bits
     auto run = [&](auto *tag) {
         using T = std::remove_pointer_t<decltype(tag)>;
         const ConvArgs<T> a = {(const T *)xbc, (const T *)w, (const T *)b, (const T *)window_in, (T *)window_out, (T *)xo, (T *)Bo, (T *)Co, ld, Cx, Cb};

@@ -451,7 +451,7 @@ bool ssd_any_wanted(const CarryTab &t, int H, int n) {
 bool ssd_any_supported(const CarryTab &t, int H, int P, int n) {
     long long chunks = 0;
     for (int s = 0; s < t.nseq; ++s) chunks += ceil_div(t.len[s], kQ);
-    return n <= 128 && chunks / 32 + t.nseq <= 65535 && (double)chunks * H * P * n * 4 <= (double)kMostStates && chunks * H * ceil_div(P, kSlab) < (1 << 24);
+    return n <= 128 && chunks / 32 + t.nseq <= 65535 && (double)chunks * H * P * n * 4 <= (double)kMostStates && chunks * H * ceil_div(P, kSlab) <= (1 << 24) - kXcd;
 }
 
 size_t ssd_any_ws(const CarryTab &t, int H, int P, int n) { return plan_any(t, H, P, n).bytes(); }
