@@ -127,23 +127,23 @@ def _heads(H, G, some):
     return [h * G // H for h in some]
 
 
-def _check_fine(seqs, x, dt, A, B, C, D, pool, slots, fresh, got, after, roundings, some=None):
-    """Heads `some` (None: all) of a packed scan: states as fp32 sums -- two pieces of bf16 leave out 2^-16 of a term at most --, outputs with `roundings` of
-    what they sum to bf16 and their own."""
+def _check_fine(seqs, x, dt, A, B, C, D, pool, slots, fresh, got, after, roundings, some=None, chans=None, pieces=True):
+    """Heads `some` and their channels `chans` (None: all) of a packed scan: states as fp32 sums (`pieces`: whose terms go in as two bf16 numbers at
+    least, which leave out 2^-16 of one), outputs with `roundings` to bf16 of what they sum, and their own."""
     H, G = x.shape[1], B.shape[1]
-    some = list(range(H)) if some is None else some
+    some, chans = list(range(H)) if some is None else some, list(range(x.shape[2])) if chans is None else chans
     gs = _heads(H, G, some)
-    X, DT, AA, BB, CC = np64(x[:, some]), np64(dt[:, some]), np64(A[some]), np64(B[:, gs]), np64(C[:, gs])
-    DD, r, half = None if D is None else np64(D[some]), 0, HALF[x.dtype]
+    X, DT, AA, BB, CC = np64(x[:, some][:, :, chans]), np64(dt[:, some]), np64(A[some]), np64(B[:, gs]), np64(C[:, gs])
+    DD, r, half = None if D is None else np64(D[some]), 0, HALF[got.dtype]
     for i, s in enumerate(seqs):
         at = slice(r, r + s[0] + s[1])
         r = at.stop
-        S0 = np64(pool[slots[i], some]) if pool is not None and not (fresh is not None and fresh[i]) else np.zeros((len(some), x.shape[2], B.shape[2]))
+        S0 = np64(pool[slots[i], some][:, chans]) if pool is not None and not (fresh is not None and fresh[i]) else np.zeros((len(some), len(chans), B.shape[2]))
         y, S, ey, eS, my, m = _fine_scan(X[at], DT[at], AA, BB[at], CC[at], DD, S0)
         inner = ey + roundings * 2.0 ** -8 * (1 + 2.0 ** -7) * my
-        base._within(got[at][:, some], y, inner + half * (np.abs(y) + inner) + 1e-37, "y of sequence %d" % i)
+        base._within(got[at][:, some][:, :, chans], y, inner + half * (np.abs(y) + inner) + 1e-37, "y of sequence %d" % i)
         if after is not None:
-            base._within(after[slots[i], some], S, eS + (2.0 ** -16 * m if x.dtype == BF16 else 0) + 1e-37, "state of sequence %d" % i)
+            base._within(after[slots[i], some][:, chans], S, eS + (2.0 ** -16 * m if pieces else 0) + 1e-37, "state of sequence %d" % i)
 
 
 RESETS = [(BF16, 64, 4, 64, 64), (BF16, 32, 2, 128, 64), (BF16, 8, 2, 128, 64), (F32, 8, 2, 64, 64), (BF16, 6, 6, 24, 40)]
@@ -165,7 +165,8 @@ def test_scan_varlen_goes_on_behind_tokens_that_reset_a_head(size, dtype, H, G, 
     pool = base._rand(torch.Generator().manual_seed(2), len(seqs), H, P, n)
     state = base._dev(pool)
     y = strd.ssd_prefill_varlen(*(base._dev(t) for t in (x, dt, A, B, C)), seqs, base._dev(D), state=state)
-    _check_fine(seqs, x, dt, A, B, C, D, pool, list(range(len(seqs))), None, y, state, 0 if dtype == F32 else 2, some=list(range(0, H, max(1, H // 8))))
+    _check_fine(seqs, x, dt, A, B, C, D, pool, list(range(len(seqs))), None, y, state, 0 if dtype == F32 else 2, some=list(range(0, H, max(1, H // 8))),
+                pieces=dtype == BF16)
 
 
 @pytest.mark.parametrize("H,G,n", [(64, 4, 64), (32, 2, 128)])
