@@ -513,8 +513,9 @@ int strd_cache_evict(const float *w, int T, int K, int first, int last, const st
  *   bf16 in an output (a third of what earlier tokens left, where each of heads 4 i to 4 i + 3 decays by 2^-12 or more in every 32 tokens of a stretch),
  *   none in a state; sums of more than 2^79 in a state may leave fp32.  Small batches of them run in fp32, as does
  *   every other shape and type, those at any alignment.  Final states are fp32 sums either way.  Where sequences are cut follows from
- *   the whole batch, and with it the last bits of a result.  Values that are not finite stay in their own sequence; there they show in
- *   every later output of their channel (dt: of their head) and, as tokens are weighed in blocks, up to 63 tokens earlier.
+ *   the whole batch, and with it the last bits of a result (later decays of a head show in those of its earlier outputs).  Values that are not finite
+ *   stay in their own sequence.  There one of x or of a state shows in every later output of its channel, one of dt of its head, one of B of all heads of its
+ *   group, and, as tokens are weighed in blocks, up to 63 tokens earlier; one of C shows in its group's outputs at its own token.
  * ssd_decode_steps -- strd_ssd_decode_step for one token each of `batch` sequences: x, y [dev] [batch, H, P], dt [batch, H],
  *   B, C [batch, G, n], states in the pool.  batch <= 65535, H * P <= 2^24, H * P * n <= 2^30 (else STRD_EUNSUPPORTED).
  *

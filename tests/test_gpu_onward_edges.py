@@ -187,3 +187,50 @@ def test_scan_varlen_a_reset_does_not_cost_the_steps_that_remember_a_rounding(H,
     seqs = [(T, 0, 0)]
     y = strd.ssd_prefill_varlen(*(base._dev(t) for t in (x, dt, A, B, C)), seqs)
     _check_fine(seqs, x, dt, A, B, C, None, None, [0], None, y, None, 1)
+
+
+# ------------------------------------------------------------------ packed scans: values that are not finite, and where they show
+@pytest.mark.parametrize("dtype,H,P,G,n", [(BF16, 64, 64, 4, 64), (BF16, 32, 64, 2, 128), (BF16, 8, 64, 2, 128), (F32, 4, 32, 2, 16), (BF16, 8, 64, 8, 64), (F32, 4, 20, 2, 160)])
+@pytest.mark.parametrize("what", ["B", "C", "dt", "state"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_scan_varlen_where_values_that_are_not_finite_show(what, value, dtype, H, P, G, n):
+    """One in B: all channels of its group's heads, one in dt: of its head, one in a state: its channel, from its token on and up to 63 tokens before (a state:
+    everywhere), and their final states; one in C: its group's heads at its token.  Everything else has the bits that it has without -- but for earlier outputs of a head whose dt is not finite:
+    how many pieces a state between segments is made of follows from the decays behind it, so those are off by a rounding at most."""
+    base._say("scan not finite", what, value, dtype, H, P, G, n)
+    seqs, at = [(700, 0, 0), (40, 0, 0), (900, 5, 0)], 650
+    x, dt, A, B, C, D = base._scan_case(1645, H, P, G, n, dtype, slow=True)
+    pool = base._rand(torch.Generator().manual_seed(1), 3, H, P, n)
+    want_S = base._dev(pool)
+    want = strd.ssd_prefill_varlen(*(base._dev(t) for t in (x, dt, A, B, C)), seqs, base._dev(D), state=want_S)
+    g, h, p, c = 1, H - 1, 3, 5
+    mine = torch.zeros(H, P, dtype=torch.bool)     # heads and channels that it reaches
+    if what in ("B", "C"):
+        (B if what == "B" else C)[at, g, c] = value
+        mine[g * H // G:(g + 1) * H // G] = True
+    elif what == "dt":
+        dt[at, h] = value
+        mine[h] = True
+    else:
+        pool[0, h, p, c], at = value, 0
+        mine[h, p] = True
+    state = base._dev(pool)
+    y = strd.ssd_prefill_varlen(*(base._dev(t) for t in (x, dt, A, B, C)), seqs, base._dev(D), state=state)
+    fine, yes = torch.isfinite(y).cpu(), mine[None].expand(700, H, P)
+    last = at + 1 if what == "C" else 700
+    assert not fine[at:last][yes[at:last]].any()
+    touched = torch.zeros(y.shape, dtype=torch.bool)
+    touched[at if what == "C" else max(0, at - 63):last] = mine
+    same = (y == want).cpu()
+    if what == "dt":
+        # two pieces of bf16 or three are 2^-16 of a term apart, which is rounded as part of a state and of the output either way
+        my = _fine_scan(*(np64(t) for t in (x[:at, h:], dt[:at, h:], A[h:], B[:at, -1:], C[:at, -1:], D[h:], pool[0, h:])))[4][:at - 63, 0]
+        was = np64(want[:at - 63, h])
+        assert (np.abs(np64(y[:at - 63, h]) - was) <= 2 * HALF[dtype] * np.abs(was) + (2.0 ** -16 + 2 * HALF[dtype]) * my).all()
+        touched[:at, h] = True
+    assert same[~touched].all()
+    fine_S, same_S, reached = torch.isfinite(state).cpu(), (state == want_S).cpu(), torch.zeros(state.shape, dtype=torch.bool)
+    if what != "C":
+        reached[0] = mine[..., None]
+        assert not fine_S[0].all(-1)[mine].any()
+    assert same_S[~reached].all()
