@@ -66,6 +66,52 @@ def test_scan_of_segments_in_parts(name, style):
                       [0, 3, 4, 21, 42, 63])
 
 
+@pytest.mark.parametrize("lens,H,G,n", [([9000, 300], 128, 8, 64), ([20000, 700], 64, 4, 128)])
+@pytest.mark.parametrize("style", ["forget", "mixed"])
+def test_scan_of_segments_in_parts_keeps_what_is_not_finite(lens, H, G, n, style):
+    """... in every later output of its channel and in its final state, also where what a part leaves behind it is not worked out; in no other."""
+    base._say("scan parts not finite", lens, H, G, n, style)
+    plan = plans.scan_plan(lens, H, n)
+    assert plan["segments"][0] > 3 and plan["parts"][0] > 1
+    x, dt, A, B, C, D = _long_scan(lens, H, 64, G, n, BF16, style)
+    seqs, pool = [(t, 0, 0) for t in lens], torch.zeros((len(lens), H, 64, n), device=DEV)
+    want_S, state = pool.clone(), pool.clone()
+    want = strd.ssd_prefill_varlen(x, dt, A, B, C, seqs, D, state=want_S)
+    odd = [(100, 5, 37, float("nan")), (lens[0] // 2, H - 2, 2, float("inf")), (lens[0] + 200, 6, 63, float("-inf"))]
+    touched, reached = torch.zeros(want.shape, dtype=torch.bool, device=DEV), torch.zeros(pool.shape, dtype=torch.bool, device=DEV)
+    for t, h, p, value in odd:
+        x[t, h, p] = value
+    y = strd.ssd_prefill_varlen(x, dt, A, B, C, seqs, D, state=state)
+    for t, h, p, value in odd:
+        s = int(t >= lens[0])
+        end = lens[0] + s * lens[1]
+        assert not torch.isfinite(y[t:end, h, p]).any() and not torch.isfinite(state[s, h, p]).any()
+        touched[max(t - 63, s * lens[0]):end, h, p] = True
+        reached[s, h, p] = True
+    assert (y == want)[~touched].all() and (state == want_S)[~reached].all()
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_random_long_scan(seed):
+    rng = np.random.default_rng(700 + seed)
+    H, G, n = [(128, 8, 64), (64, 4, 128), (24, 3, 128), (96, 8, 64), (32, 8, 128), (16, 2, 64)][seed % 6]
+    left, lens = int(2 ** rng.uniform(12, 14.5)), []
+    while left > 0 and len(lens) < 9:
+        lens.append(left if rng.random() < 0.4 or len(lens) == 8 else int(rng.integers(0, left + 1)))
+        left -= lens[-1]
+    style, fresh = str(rng.choice(["forget", "some", "remember", "mixed"])), [bool(rng.random() < 0.3) for _ in lens]
+    plan = plans.scan_plan(lens, H, n)
+    base._say("random long scan", seed, lens, H, G, n, style, plan["parts"], plan["segments"])
+    assert not plans.chunks_wanted(lens, H, n) and plan["bytes"] == _scan_bytes(lens, H, 64, G, n, BF16)
+    x, dt, A, B, C, D = _long_scan(lens, H, 64, G, n, BF16, style)
+    pool = torch.randn((len(lens) + 2, H, 64, n), generator=torch.Generator(device=DEV).manual_seed(seed), device=DEV)
+    slots, out = rng.permutation(len(lens) + 2)[:len(lens)].tolist(), torch.full_like(pool, 7.0)
+    y = strd.ssd_prefill_varlen(x, dt, A, B, C, [(t, 0, 0) for t in lens], D, state=pool, state_out=out, slots=slots, fresh=fresh)
+    some = sorted(set(int(h) for h in rng.integers(0, H, 6)))
+    edges._check_fine([(t, 0, 0) for t in lens], x, dt, A, B, C, D, pool, slots, fresh, y, out, 1 if style in ("remember", "mixed") else 2, some,
+                      sorted(set(int(p) for p in rng.integers(0, 64, 6))))
+
+
 @pytest.mark.parametrize("lens,H,G,n", [([949, 398, 704, 129, 1240, 73], 128, 8, 128), ([1200, 395, 40], 64, 4, 64), ([2000, 31], 32, 2, 128)])
 @pytest.mark.parametrize("style", ["forget", "mixed"])
 def test_scan_final_states_are_fp32_sums(lens, H, G, n, style):
@@ -182,4 +228,17 @@ def test_tree_over_long_caches_of_other_shapes(dtype, T, m, Hq, Hkv, d, join, ca
     plan = plans.tree_plan(T, m, Hq, Hkv, d)
     assert d % 4 or plans.waves_of_the_join(plan["general"]) == join
     assert plan["bytes"] == binding.lib().strd_attn_tree_step_workspace(T, m, Hq, Hkv, d, 1) or dtype == F32
+    _long_tree(T, m, Hq, Hkv, d, dtype, cap, slopes, pos)
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_random_tree_over_a_long_cache(seed):
+    rng = np.random.default_rng(900 + seed)
+    Hkv = int(rng.choice([1, 2, 4, 8]))
+    Hq, d, m = Hkv * int(rng.integers(1, 9)), int(rng.choice([64, 96, 128])), int(rng.integers(1, 65))
+    T, dtype = int(2 ** rng.uniform(11, 15)), F32 if seed % 4 == 3 else BF16
+    cap, slopes, pos = float(rng.choice([0.0, 1.0, 30.0, 50.0])), bool(rng.random() < 0.5), bool(rng.random() < 0.5)
+    if dtype == F32:
+        T //= 4
+    base._say("random long tree", seed, T, m, Hq, Hkv, d, dtype, cap, slopes, pos, plans.tree_plan(T, m, Hq, Hkv, d))
     _long_tree(T, m, Hq, Hkv, d, dtype, cap, slopes, pos)
