@@ -537,7 +537,8 @@ int strd_cache_evict(const float *w, int T, int K, int first, int last, const st
  *   visible (bits from m on are not looked at).  1 <= m <= 64, T >= 0 (0: no cache needed).  A node that sees nothing gets zeros; what a node does
  *   not see does not reach it, values that are not finite included.  Scores with cap and slopes as in attn_prefill_varlen above; pos [dev] [T + m]
  *   int32, the cache's rows first; NULL: a row's number, and for a node T + the number of other nodes that it sees (in a tree: its depth).
- *   d <= 256, Hkv <= 65535, m * Hq <= 2^21 (else STRD_EUNSUPPORTED), Hq % Hkv == 0, T <= 2^30.  Workspace [dev], 16-byte aligned: strd_attn_tree_step_workspace bytes (STRD_EWORKSPACE).  Deterministic.
+ *   d <= 256, Hkv <= 65535, m * Hq <= 2^21 (else STRD_EUNSUPPORTED), Hq % Hkv == 0, T <= 2^30.  Workspace [dev], 16-byte aligned:
+ *   strd_attn_tree_step_workspace bytes (STRD_EWORKSPACE).  Deterministic.
  * tree_mask -- mask of a tree: parent[i] in [-1, i) is node i's parent (-1: it hangs on the cache's last row); node i sees itself and its
  *   ancestors.  Host-only.  STRD_EINVAL for any other parent or m outside 1..64.
  *
