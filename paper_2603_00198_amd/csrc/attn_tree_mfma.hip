@@ -6,7 +6,8 @@
 //    weight of 0 takes a value out of the second product only if it is finite: in chunks with nodes the values are looked at when they have landed in
 //    LDS, and those that are not finite are taken out and added at the end, row by row.
 //  * A row's softmax has a reference that moves when eight of its weights add up to more than 2^8, or at its first keys.
-// 64 nodes of 32 heads behind 131627 rows, capped and biased: 175 us for 541 MB and 138 GFLOP (790 TFLOP/s), then 11 to join 32 splits; the matrix units are at
+// 64 nodes of 32 heads behind 131627 rows, capped and biased: 178 us for 541 MB and 138 GFLOP (775 TFLOP/s; 175 before capped
+// references far from zero were taken off the scores; other shapes took the same), then 11 to join 32 splits; the matrix units are at
 // work 35 % of the time and the vector units 50 % (10 instructions a score, one of them an exponential), at 2.0 GHz of 2.4.  Neither of the two alone bounds
 // it: fewer instructions in the cap, other priorities of the waves and other chunks all take 175 +- 2.  Few rows are bound by HBM: 8 nodes 110 us, 4.9 TB/s.
 #include <algorithm>
