@@ -193,6 +193,11 @@ __device__ __forceinline__ strd_bf16x8 tr_pair(strd_s16x4 lo, strd_s16x4 hi) {
                                    4, 5, 6, 7);
 }
 
+// log2 of a token's decay as the scans on the matrix cores add it up inside a step.  The weights of tokens behind one that resets the head are differences of
+// such sums, so as much as leaves nothing in fp32 is enough (2^-150, and what a state's unit takes off it); behind 1e6 they would be off by a sixteenth.
+// (NaN stays.)
+__device__ __forceinline__ float step_decay(float l) { return l < -200.f ? -200.f : l; }
+
 // Workgroup barrier that orders LDS traffic only.  __syncthreads() also fences global memory,
 // which on gfx9 means waiting for every outstanding vector-memory operation of the wave -- all
 // the asynchronous copies requested steps ahead and every global store still in flight.  Here

@@ -408,7 +408,7 @@ __device__ __forceinline__ void helper_wave(Lds<NS> &lds, const bf16_t *__restri
     // scan of dt*A of `step` from the dt ring, the key factors of (b) and the weights of (e)
     auto make_scan = [&](int step, float raw) __attribute__((always_inline)) {
         const float dv = (step * kQ + lane < T) ? raw : 0.f;
-        const float inc = wave_inclusive_scan_f32(dv * Al2);
+        const float inc = wave_inclusive_scan_f32(step_decay(dv * Al2));
         typename L::Scan &m = lds.scan[step % 3];
         m.ell[lane] = inc;
         m.dtv[lane] = dv;

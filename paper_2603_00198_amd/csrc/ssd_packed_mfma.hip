@@ -30,7 +30,6 @@ namespace strd {
 namespace {
 
 constexpr float kGone = -150.f;     // log2 of a decay that leaves nothing in fp32
-constexpr float kReset = -200.f;    // ... nor after a unit below has been taken off it
 constexpr float kApart = 48.f;      // log2 of how far a state's unit may be from 1
 constexpr float kForgets = -12.f;  // log2 of the decay over every step of a segment from which on w x is taken in one piece
 
@@ -312,10 +311,7 @@ __device__ __forceinline__ void helper_wave(LdsP<NS> &lds, const PackArgs &a, in
     };
     auto make_scan = [&](int k, int i, float raw) __attribute__((always_inline)) {
         const float dv = row0 + i * kQ + j < row_end ? raw : 0.f;
-        float inc = dv * Al2[k];  // inclusive prefix sum over the 32 lanes of a head
-        // The weights of tokens behind one that resets the head are differences of these sums: as much as leaves nothing is enough, and what is behind 1e6
-        // would be off by a sixteenth.  (NaN stays.)
-        inc = inc < kReset ? kReset : inc;
+        float inc = step_decay(dv * Al2[k]);  // inclusive prefix sum over the 32 lanes of a head
 #define STRD_DPP_FADD(ctrl, row_mask) \
     inc += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, inc), ctrl, row_mask, 0xF, true))
         STRD_DPP_FADD(0x111, 0xF);  // row_shr:1

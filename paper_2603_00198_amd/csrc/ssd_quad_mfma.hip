@@ -296,7 +296,7 @@ __device__ __forceinline__ void helper_wave(LdsQ<NS> &lds, const QuadArgs &a, in
     int life[2] = {0, 0};
     auto make_scan = [&](int k, int i, float raw) __attribute__((always_inline)) {
         const float dv = (tok0 + i * kQ + j < a.T) ? raw : 0.f;
-        float inc = dv * Al2[k];  // inclusive prefix sum over the 32 lanes of a head
+        float inc = step_decay(dv * Al2[k]);  // inclusive prefix sum over the 32 lanes of a head
 #define STRD_DPP_FADD(ctrl, row_mask) \
     inc += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, inc), ctrl, row_mask, 0xF, true))
         STRD_DPP_FADD(0x111, 0xF);  // row_shr:1

@@ -601,7 +601,7 @@ __device__ __forceinline__ void helper_wave(LdsS<NS, NC, NH> &lds, const SegArgs
     // of (d); returns the total log2 decay of the step
     auto make_scan = [&](int hh, int i, float raw) __attribute__((always_inline)) -> float {
         const float dv = (tok0 + i * kQ + lane < a.T) ? raw : 0.f;
-        const float inc = wave_inclusive_scan_f32(dv * Al2[hh]);
+        const float inc = wave_inclusive_scan_f32(step_decay(dv * Al2[hh]));
         typename L::Scan &m = lds.scan[hh][i & 1];
         const float tot = read_lane_f32(inc, kQ - 1);
         m.ell[lane] = inc;
